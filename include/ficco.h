@@ -535,6 +535,124 @@ double ficco_ideal_overlap_us(double t_comm_us, double t_gemm_us, int n);
 int ficco_gemm_static(int64_t M, int64_t K, int64_t N, const void *A_dev, const void *W_dev, void *C_dev,
                       void *stream);
 
+/*
+ * Operators around the pair: what a layer does next to the products above, on operands that are already in device memory.
+ * They need no plan. Options and sizes are in a struct that the caller fills (zero is every field's default) and may keep;
+ * nothing is kept between calls, no device memory is allocated, and the work is enqueued on `stream` (hipStream_t), so that
+ * the caller may capture it into a graph. A workspace is device memory of the caller's, of at least the bytes that the
+ * operator's _workspace function gives for the same struct (NULL where that is 0); it holds nothing between calls, and
+ * calls that may run at the same time need one each. All matrices are row-major. Every pointer must be device memory of
+ * the current device (FICCO_ERR_ARG), and those of bf16 matrices and of workspaces 16-byte aligned, other 32-bit values 4-byte (FICCO_ERR_ARG).
+ * Inputs and outputs must not overlap except where it is said. Each result is rounded once, from fp32 to its type, to
+ * nearest even; sums are in fp32 and in an order that depends on the sizes only, so that equal calls give equal bits.
+ */
+typedef enum ficco_type { FICCO_BF16 = 0, FICCO_F32 = 1 } ficco_type;
+
+typedef enum ficco_activation {
+    FICCO_ACT_NONE = 0,
+    FICCO_ACT_RELU = 1,
+    FICCO_ACT_GELU = 2,          /* z Phi(z), Phi the normal distribution function                        */
+    FICCO_ACT_GELU_TANH = 3,     /* z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))                          */
+    FICCO_ACT_SILU = 4           /* z / (1 + exp(-z))                                                      */
+} ficco_activation;
+
+typedef enum ficco_weight_layout {
+    FICCO_WEIGHT_KN = 0,         /* W [K,N], as everywhere else in this interface                          */
+    FICCO_WEIGHT_NK = 1          /* W [N,K], k contiguous: the layout the kernels read, nothing is re-laid out in the forward */
+} ficco_weight_layout;
+
+/*
+ * A product with bias, activation and residual in its epilogue:
+ *   z = A W + bias,  pre = bf16(z),  C = act(z) + residual       A [M,K], W [K,N] or [N,K], C, pre, residual [M,N] bf16
+ * bias [N] (bf16 or fp32), residual and pre may be NULL; residual may be C itself. The activation sees z in fp32.
+ * Gradients, from dC [M,N] bf16 and the stored pre (not read, and may be NULL, with FICCO_ACT_NONE):
+ *   dZ = dC act'(pre),  dbias = column sums of dZ (fp32),  dA = dZ W^T,  dW = A^T dZ (both bf16, dense, dW in W's layout)
+ * each of dA, dW, dbias NULL if it is not wanted; the residual's gradient is dC. dZ is rounded to bf16 for the two products
+ * (they are bf16 products) and not for dbias. act' of FICCO_ACT_RELU at 0 is 0.
+ * Row strides in elements, 0 = dense: lda of A, ldc of C and of dC, ld_residual, ld_pre; multiples of 8, at least the row's
+ * length, lda and ldc at most 2^22. Shape rules (FICCO_ERR_SHAPE): 0 <= M < 2^31, K % 64 == 0, N % 8 == 0, K and N
+ * positive and at most 2^22; the backward pass needs M <= 2^22. With M == 0 nothing is read; dW and dbias are zero.
+ * Workspace: the forward of a [K,N] weight keeps its re-laid out copy there (K N 2 bytes) unless the product is small; the
+ * backward keeps dZ and the operands that its products need with another order of their values.
+ */
+typedef struct ficco_linear_t {
+    int64_t M, K, N;
+    int64_t lda, ldc, ld_residual, ld_pre;
+    int32_t weight_layout;       /* ficco_weight_layout */
+    int32_t activation;          /* ficco_activation */
+    int32_t bias_type;           /* ficco_type */
+    int32_t reserved;            /* 0 */
+} ficco_linear_t;
+
+int ficco_linear_workspace(const ficco_linear_t *op, int backward, int64_t *bytes);
+int ficco_linear(const ficco_linear_t *op, const void *A, const void *W, const void *bias, const void *residual, void *pre,
+                 void *C, void *workspace, int64_t workspace_bytes, void *stream);
+int ficco_linear_backward(const ficco_linear_t *op, const void *A, const void *W, const void *pre, const void *dC, void *dA,
+                          void *dW, void *dbias, void *workspace, int64_t workspace_bytes, void *stream);
+
+/*
+ * What stands between one block of a layer and the next (behind ficco_rs_reduce, in front of the next gather): the norm
+ * behind a block, its gate, the scaled residual stream and the norm in front of the next block, in one pass over the rows.
+ *   n = post_weight * block / sqrt(mean(block^2) + eps)      (n = block if post_weight is NULL)
+ *   y = residual_scale * x + gate * n                        (gate NULL: 1)
+ *   h = pre_weight * y / sqrt(mean(y^2) + eps)               (h and pre_weight both NULL: not computed)
+ * x, y [rows,width] of stream_type (y may be x itself), block, h [rows,width] bf16; the weights [width] and the gate
+ * [width], or with gate_rows > 0 [ceil(rows/gate_rows),width] with row r / gate_rows for row r, of param_type. h is the norm
+ * of y as computed, before y is rounded.
+ * Gradients, from dy of stream_type (NULL: 0) and dh bf16 (NULL, with dpre_weight: h was not used), with y as stored:
+ *   dY = dy + (the norm's part of dh);  dx = residual_scale * dY (stream_type; NULL: not wanted; may be dy itself)
+ *   dblock bf16, and fp32 sums over the rows: dpost_weight [width], dgate of the gate's shape, dpre_weight [width]
+ * each given or NULL; those of NULL parameters must be NULL. dblock and dgate need block (FICCO_ERR_ARG).
+ * Shape rules (FICCO_ERR_SHAPE): 0 <= rows < 2^31, width % 8 == 0, 8 <= width <= 16384, gate_rows >= 0. With no rows
+ * nothing is read, and the sums are zero. eps >= 0 and finite (FICCO_ERR_ARG).
+ */
+typedef struct ficco_residual_norm_t {
+    int64_t rows, width, gate_rows;
+    int32_t stream_type, param_type;     /* ficco_type */
+    float residual_scale, eps;
+} ficco_residual_norm_t;
+
+int ficco_residual_norm_workspace(const ficco_residual_norm_t *op, int64_t *bytes);      /* of the backward; the forward needs none */
+int ficco_residual_norm(const ficco_residual_norm_t *op, const void *x, const void *block, const void *post_weight,
+                        const void *gate, const void *pre_weight, void *y, void *h, void *stream);
+int ficco_residual_norm_backward(const ficco_residual_norm_t *op, const void *y, const void *block, const void *post_weight,
+                                 const void *gate, const void *pre_weight, const void *dy, const void *dh, void *dx,
+                                 void *dblock, void *dpost_weight, void *dgate, void *dpre_weight, void *workspace,
+                                 int64_t workspace_bytes, void *stream);
+
+/*
+ * Counts of tokens per expert, and the loss that keeps a router from preferring a few. Tokens go in groups of group_tokens
+ * (0: all are one group; the last one may be shorter): a sequence, a batch, or the tokens of one peer, for which a row of
+ * counts is that peer's row of ficco_plan_grouped's `rows`.
+ *   counts[g][e]    int32: how often expert e is among the ids of group g's valid tokens
+ *   group_valid[g]  int32: valid tokens of group g
+ *   loss            fp32: coefficient * experts / groups * sum over g, e of counts[g][e] / (top_k n_g) * P[g][e], with n_g =
+ *                   group_valid[g], P[g][e] the mean of softmax(logits)[t][e] over the group's valid tokens; a group
+ *                   without any adds nothing. Even routing gives `coefficient`. NULL: counts only (logits may be NULL too)
+ * logits [tokens,experts] (bf16 or fp32, row stride ld_logits, 0 = dense, at least experts), ids [tokens,top_k] int32; an id outside
+ * [0, experts) is a dropped slot and counted nowhere, the same id twice counts twice. valid [tokens] bytes, 0 = padding (NULL: all are
+ * valid); the logits of padding are not looked at. A logit of -inf is an expert that the token may not use; a valid token
+ * with nothing but -inf has no probabilities and adds nothing to P, but is counted in group_valid.
+ * The gradient: dlogits of logits' type and stride = dloss[0] (fp32, NULL: 1) times d loss / d logits, through the
+ * probabilities (counts are constants); 0 for padding. It takes counts and group_valid as the forward wrote them. dlogits may be logits itself.
+ * Shape rules (FICCO_ERR_SHAPE): 0 <= tokens < 2^31, 1 <= experts <= 1024, 1 <= top_k <= 64, group_tokens >= 0, at most
+ * 2^20 groups. With no tokens there are no groups: the loss is 0 and nothing else is written.
+ */
+typedef struct ficco_expert_balance_t {
+    int64_t tokens, group_tokens, ld_logits;
+    int32_t experts, top_k;
+    int32_t logits_type;         /* ficco_type */
+    float coefficient;
+} ficco_expert_balance_t;
+
+int ficco_expert_balance_workspace(const ficco_expert_balance_t *op, int64_t *bytes);    /* of the forward; the backward needs none */
+int ficco_expert_balance(const ficco_expert_balance_t *op, const void *logits, const void *ids, const void *valid,
+                         void *counts, void *group_valid, void *loss, void *workspace, int64_t workspace_bytes,
+                         void *stream);
+int ficco_expert_balance_backward(const ficco_expert_balance_t *op, const void *logits, const void *valid,
+                                  const void *counts, const void *group_valid, const void *dloss, void *dlogits,
+                                  void *stream);
+
 void ficco_destroy(ficco_plan_t *plan);      /* waits for the plan's runs, frees what it owns */
 
 const char *ficco_strerror(int status);

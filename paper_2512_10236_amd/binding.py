@@ -25,6 +25,9 @@ FICCO_MODE_PAIR, FICCO_MODE_GEMM_ONLY, FICCO_MODE_COPY_ONLY, FICCO_MODE_INDEPEND
  FICCO_OPT_COPY_BACKEND, FICCO_OPT_LINKS, FICCO_OPT_PACKING, FICCO_OPT_REPEAT,
  FICCO_OPT_TILE_GROUP, FICCO_OPT_TILE_COLUMN_LISTS, FICCO_OPT_SOURCE_LAYOUT) = range(16)
 FICCO_LAYOUT_ROW_MAJOR, FICCO_LAYOUT_K_SLICED, FICCO_LAYOUT_ROW_MAJOR_HOST = 0, 1, 2
+FICCO_BF16, FICCO_F32 = 0, 1
+FICCO_ACT_NONE, FICCO_ACT_RELU, FICCO_ACT_GELU, FICCO_ACT_GELU_TANH, FICCO_ACT_SILU = range(5)
+FICCO_WEIGHT_KN, FICCO_WEIGHT_NK = 0, 1
 FICCO_COPY_AUTO, FICCO_COPY_STREAM, FICCO_COPY_ENGINES = 0, 1, 2
 (FICCO_TILE_AUTO, FICCO_TILE_256x256, FICCO_TILE_128x128, FICCO_TILE_256x128, FICCO_TILE_128x256,
  FICCO_TILE_64x256, FICCO_TILE_32x256, FICCO_TILE_128x128_DEEP, FICCO_TILE_128x192,
@@ -69,9 +72,27 @@ class ficco_losses_t(C.Structure):
         return {k: getattr(self, k) for k, _ in self._fields_}
 
 
+class ficco_linear_t(C.Structure):
+    _fields_ = [("M", C.c_int64), ("K", C.c_int64), ("N", C.c_int64), ("lda", C.c_int64), ("ldc", C.c_int64),
+                ("ld_residual", C.c_int64), ("ld_pre", C.c_int64), ("weight_layout", C.c_int32),
+                ("activation", C.c_int32), ("bias_type", C.c_int32), ("reserved", C.c_int32)]
+
+
+class ficco_residual_norm_t(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int64), ("gate_rows", C.c_int64), ("stream_type", C.c_int32),
+                ("param_type", C.c_int32), ("residual_scale", C.c_float), ("eps", C.c_float)]
+
+
+class ficco_expert_balance_t(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("group_tokens", C.c_int64), ("ld_logits", C.c_int64), ("experts", C.c_int32),
+                ("top_k", C.c_int32), ("logits_type", C.c_int32), ("coefficient", C.c_float)]
+
+
 EXPORTS = ["ficco_plan", "ficco_plan_grouped", "ficco_plan_pieces", "ficco_plan_set_slice_widths", "ficco_plan_slices", "ficco_plan_chain", "ficco_plan_set", "ficco_plan_set_arrival", "ficco_plan_info", "ficco_plan_arrival",
            "ficco_pack_weight", "ficco_run", "ficco_gemm_static", "ficco_graph_capture", "ficco_graph_launch", "ficco_rs_reduce", "ficco_query_stats", "ficco_query_spans", "ficco_profile_losses",
            "ficco_pick_schedule", "ficco_pick_schedule_rs", "ficco_pick_schedule_any", "ficco_pick_schedule_layout", "ficco_pick_slice_widths", "ficco_static_descriptors", "ficco_ideal_overlap_us", "ficco_destroy",
+           "ficco_linear_workspace", "ficco_linear", "ficco_linear_backward", "ficco_residual_norm_workspace", "ficco_residual_norm", "ficco_residual_norm_backward",
+           "ficco_expert_balance_workspace", "ficco_expert_balance", "ficco_expert_balance_backward",
            "ficco_strerror", "ficco_last_hip_error", "ficco_version"]
 
 _lib = None
@@ -121,6 +142,17 @@ def load():
     lib.ficco_static_descriptors.argtypes = [i64, i64, i64, dp, dp]
     lib.ficco_ideal_overlap_us.argtypes = [C.c_double, C.c_double, C.c_int]
     lib.ficco_ideal_overlap_us.restype = C.c_double
+    i64p = C.POINTER(i64)
+    lin, norm, bal = C.POINTER(ficco_linear_t), C.POINTER(ficco_residual_norm_t), C.POINTER(ficco_expert_balance_t)
+    lib.ficco_linear_workspace.argtypes = [lin, C.c_int, i64p]
+    lib.ficco_linear.argtypes = [lin] + [vp] * 7 + [i64, vp]
+    lib.ficco_linear_backward.argtypes = [lin] + [vp] * 8 + [i64, vp]
+    lib.ficco_residual_norm_workspace.argtypes = [norm, i64p]
+    lib.ficco_residual_norm.argtypes = [norm] + [vp] * 8
+    lib.ficco_residual_norm_backward.argtypes = [norm] + [vp] * 13 + [i64, vp]
+    lib.ficco_expert_balance_workspace.argtypes = [bal, i64p]
+    lib.ficco_expert_balance.argtypes = [bal] + [vp] * 7 + [i64, vp]
+    lib.ficco_expert_balance_backward.argtypes = [bal] + [vp] * 7
     lib.ficco_destroy.argtypes = [vp]
     lib.ficco_destroy.restype = None
     lib.ficco_strerror.argtypes = [C.c_int]
@@ -326,6 +358,80 @@ def ficco_static_descriptors(m, N, K):
 
 def ficco_ideal_overlap_us(t_comm_us, t_gemm_us, n):
     return float(load().ficco_ideal_overlap_us(t_comm_us, t_gemm_us, n))
+
+
+# ---- operators around the pair: `op` is the struct of the C interface, tensors have to be laid out as it says
+def _addr(x):
+    """Address of a buffer, a tensor or a stream, or None. A tensor's strides are the caller's to describe in `op`: one whose
+    last dimension is not contiguous cannot be."""
+    if x is None or isinstance(x, int):
+        return x
+    if hasattr(x, "data_ptr"):
+        if x.dim() and x.stride(-1) != 1 and x.size(-1) > 1:
+            raise FiccoError(FICCO_ERR_ARG, "a tensor's last dimension must be contiguous")
+        return x.data_ptr()
+    if hasattr(x, "cuda_stream"):
+        return x.cuda_stream
+    raise TypeError(type(x))
+
+
+def ficco_linear_workspace(op, backward=False):
+    """Bytes of workspace of a forward or a backward call."""
+    n = C.c_int64()
+    _ok(load().ficco_linear_workspace(op, int(backward), C.byref(n)), "ficco_linear_workspace")
+    return n.value
+
+
+def ficco_linear(op, A, W, bias, residual, pre, C_dev, workspace, workspace_bytes, stream):
+    """C = act(A W + bias) + residual (see include/ficco.h); ``op``: a :class:`ficco_linear_t`."""
+    return _ok(load().ficco_linear(op, _addr(A), _addr(W), _addr(bias), _addr(residual), _addr(pre), _addr(C_dev), _addr(workspace),
+                                   workspace_bytes, _addr(stream)), "ficco_linear")
+
+
+def ficco_linear_backward(op, A, W, pre, dC, dA, dW, dbias, workspace, workspace_bytes, stream):
+    """Gradients of :func:`ficco_linear`; any of dA, dW and dbias may be None."""
+    return _ok(load().ficco_linear_backward(op, _addr(A), _addr(W), _addr(pre), _addr(dC), _addr(dA), _addr(dW), _addr(dbias), _addr(workspace),
+                                            workspace_bytes, _addr(stream)), "ficco_linear_backward")
+
+
+def ficco_residual_norm_workspace(op):
+    """Bytes of workspace of a backward call."""
+    n = C.c_int64()
+    _ok(load().ficco_residual_norm_workspace(op, C.byref(n)), "ficco_residual_norm_workspace")
+    return n.value
+
+
+def ficco_residual_norm(op, x, block, post_weight, gate, pre_weight, y, h, stream):
+    """y = scale x + gate norm(block), h = norm(y) (see include/ficco.h); ``op``: a :class:`ficco_residual_norm_t`."""
+    return _ok(load().ficco_residual_norm(op, _addr(x), _addr(block), _addr(post_weight), _addr(gate), _addr(pre_weight), _addr(y), _addr(h),
+                                          _addr(stream)), "ficco_residual_norm")
+
+
+def ficco_residual_norm_backward(op, y, block, post_weight, gate, pre_weight, dy, dh, dx, dblock, dpost_weight, dgate, dpre_weight, workspace,
+                                 workspace_bytes, stream):
+    """Gradients of :func:`ficco_residual_norm`; those that are not wanted are None."""
+    return _ok(load().ficco_residual_norm_backward(op, _addr(y), _addr(block), _addr(post_weight), _addr(gate), _addr(pre_weight), _addr(dy), _addr(dh),
+                                                   _addr(dx), _addr(dblock), _addr(dpost_weight), _addr(dgate), _addr(dpre_weight), _addr(workspace),
+                                                   workspace_bytes, _addr(stream)), "ficco_residual_norm_backward")
+
+
+def ficco_expert_balance_workspace(op):
+    """Bytes of workspace of a forward call."""
+    n = C.c_int64()
+    _ok(load().ficco_expert_balance_workspace(op, C.byref(n)), "ficco_expert_balance_workspace")
+    return n.value
+
+
+def ficco_expert_balance(op, logits, ids, valid, counts, group_valid, loss, workspace, workspace_bytes, stream):
+    """Counts per expert and the balance loss (see include/ficco.h); ``op``: a :class:`ficco_expert_balance_t`."""
+    return _ok(load().ficco_expert_balance(op, _addr(logits), _addr(ids), _addr(valid), _addr(counts), _addr(group_valid), _addr(loss), _addr(workspace),
+                                           workspace_bytes, _addr(stream)), "ficco_expert_balance")
+
+
+def ficco_expert_balance_backward(op, logits, valid, counts, group_valid, dloss, dlogits, stream):
+    """The logits' gradient of :func:`ficco_expert_balance`."""
+    return _ok(load().ficco_expert_balance_backward(op, _addr(logits), _addr(valid), _addr(counts), _addr(group_valid), _addr(dloss), _addr(dlogits),
+                                                    _addr(stream)), "ficco_expert_balance_backward")
 
 
 def ficco_destroy(plan):

@@ -1,0 +1,437 @@
+// Counts of tokens per expert and the balance loss of a router (ficco_expert_balance and its backward). For a group g of tokens
+// with n valid ones, c_e slots of which went to expert e, and p_t = softmax(logits_t):
+//   loss = sum over g of s sum_e c_e sum_t p_te,   s = coefficient E / (G k n^2)
+//   d loss / d logits_te = s p_te (c_e - sum_j c_j p_tj)
+// Streaming work over the logits; a group of lanes has a token, V of its logits a lane. Column sums stay in registers and go to
+// memory once per chunk of tokens, so that all sums have a fixed order; counts are integers. The gradient's difference is small
+// next to its parts where a router is nearly even, so it is taken of the counts' distances from their mean, which are exact.
+#include "ficco_operators.h"
+#include "ficco_epilogue.h"
+
+namespace ficco {
+namespace {
+
+struct BalanceLaunch {
+    const void *logits;
+    const int32_t *ids;
+    const uint8_t *valid;
+    int32_t *counts, *group_valid;
+    float *loss;
+    const float *dloss;
+    void *dlogits;
+    // partial results of a chunk of tokens, where a group has several: [chunks][E], [chunks][E], [chunks]
+    float *part_p;
+    int32_t *part_c, *part_n;
+    float *terms;                 // [groups] the groups' parts of the loss
+    int64_t ld;
+    int32_t tokens, group_tokens, groups, experts, top_k;
+    int32_t per_group, chunk_tokens;       // chunk c: the (c % per_group)-th run of chunk_tokens tokens of group c / per_group
+    float coefficient;
+};
+
+static __device__ __forceinline__ float logit(const float *p) { return *p; }
+static __device__ __forceinline__ float logit(const uint16_t *p) { return __uint_as_float((uint32_t)*p << 16); }
+static __device__ __forceinline__ void put(float *p, float v) { *p = v; }
+static __device__ __forceinline__ void put(uint16_t *p, float v) { *p = (uint16_t)pack2_bf16_rne(v, 0.f); }
+
+// s of a group with n valid tokens
+static __device__ __forceinline__ float group_scale(const BalanceLaunch &a, int n)
+{
+    return n > 0 ? a.coefficient * (float)a.experts / ((float)a.groups * (float)a.top_k * (float)n * (float)n) : 0.f;
+}
+
+static __device__ __forceinline__ void chunk_range(const BalanceLaunch &a, int chunk, int &group, int &begin, int &end)
+{
+    group = chunk / a.per_group;
+    const int64_t b = (int64_t)group * a.group_tokens + (int64_t)(chunk % a.per_group) * a.chunk_tokens;
+    const int64_t e = min(min(b + a.chunk_tokens, (int64_t)(group + 1) * a.group_tokens), (int64_t)a.tokens);
+    begin = (int)min(b, (int64_t)a.tokens);
+    end = (int)max(e, (int64_t)begin);
+}
+
+// The probabilities of a token, in place of its logits: LANES lanes with V logits each, expert lane + v * LANES. A token whose
+// logits are all -inf has none.
+template <int LANES, int V>
+static __device__ __forceinline__ void softmax(float (&x)[V])
+{
+    float m = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < V; ++v) m = fmaxf(m, x[v]);
+#pragma unroll
+    for (int d = LANES / 2; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    if (m == -INFINITY) m = 0.f;
+    float s = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        x[v] = __builtin_amdgcn_exp2f((x[v] - m) * kLog2E);
+        s += x[v];
+    }
+#pragma unroll
+    for (int d = LANES / 2; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
+    const float r = s == 0.f ? 0.f : 1.0f / s;
+#pragma unroll
+    for (int v = 0; v < V; ++v) x[v] *= r;
+}
+
+// Sum over a workgroup of 4 wavefronts (256 threads) or 16, in a fixed order; thread 0 has it.
+static __device__ __forceinline__ float workgroup_sum(float v, float *s)
+{
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float t = 0.f;
+    if (threadIdx.x == 0)
+        for (int w = 0; w < (int)blockDim.x / 64; ++w) t += s[w];
+    return t;
+}
+
+// One chunk of tokens a workgroup. Where a group is one chunk (per_group == 1) it writes the group's results.
+template <class L, int LANES, int V>
+__global__ __launch_bounds__(256) void balance_kernel(BalanceLaunch a)
+{
+    constexpr int SUBS = 256 / LANES;
+    extern __shared__ float s_p[];         // [SUBS][LANES * V], then the chunk's counts
+    __shared__ float s_sum[4];
+    __shared__ int s_n;
+    int *const s_c = reinterpret_cast<int *>(s_p + SUBS * LANES * V);
+    const int E = a.experts;
+    int group, begin, end;
+    chunk_range(a, blockIdx.x, group, begin, end);
+    for (int e = threadIdx.x; e < E; e += 256) s_c[e] = 0;
+    if (threadIdx.x == 0) s_n = 0;
+    __syncthreads();
+    for (int64_t i = (int64_t)begin * a.top_k + threadIdx.x; i < (int64_t)end * a.top_k; i += 256) {
+        const int id = a.ids[i];
+        if ((unsigned)id < (unsigned)E && (!a.valid || a.valid[i / a.top_k])) atomicAdd(s_c + id, 1);
+    }
+    if (a.valid) {
+        int n = 0;
+        for (int t = begin + (int)threadIdx.x; t < end; t += 256) n += a.valid[t] != 0;
+        if (n) atomicAdd(&s_n, n);
+    }
+    const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+    if (a.loss) {
+        float p[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) p[v] = 0.f;
+        const L *logits = static_cast<const L *>(a.logits);
+        for (int64_t t = begin + sub; t < end; t += SUBS) {
+            if (a.valid && !a.valid[t]) continue;
+            float x[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = lane + v * LANES < E ? logit(logits + t * a.ld + lane + v * LANES) : -INFINITY;
+            softmax<LANES, V>(x);
+#pragma unroll
+            for (int v = 0; v < V; ++v) p[v] += x[v];
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) s_p[sub * LANES * V + lane + v * LANES] = p[v];
+    }
+    __syncthreads();
+    const int n = a.valid ? s_n : end - begin;
+    float term = 0.f;
+    for (int e = threadIdx.x; e < E; e += 256) {
+        float t = 0.f;
+        if (a.loss)
+            for (int s = 0; s < SUBS; ++s) t += s_p[s * LANES * V + e];
+        if (a.per_group == 1) {
+            a.counts[(int64_t)group * E + e] = s_c[e];
+            term += (float)s_c[e] * t;
+        } else {
+            a.part_c[(int64_t)blockIdx.x * E + e] = s_c[e];
+            if (a.loss) a.part_p[(int64_t)blockIdx.x * E + e] = t;
+        }
+    }
+    if (a.per_group == 1) {
+        if (threadIdx.x == 0) a.group_valid[group] = n;
+        if (a.loss) {
+            const float sum = workgroup_sum(term, s_sum);
+            if (threadIdx.x == 0) (a.groups == 1 ? a.loss : a.terms + group)[0] = sum * group_scale(a, n);
+        }
+    } else if (threadIdx.x == 0) {
+        a.part_n[blockIdx.x] = n;
+    }
+}
+
+// The chunks' results of one group, a workgroup each: `columns` (a power of two) threads side by side over the experts.
+__global__ __launch_bounds__(1024) void balance_group_kernel(BalanceLaunch a, int columns)
+{
+    __shared__ float s_p[1024], s_sum[16];
+    __shared__ int s_c[1024], s_n;
+    const int E = a.experts, group = blockIdx.x, col = threadIdx.x & (columns - 1), slice = threadIdx.x / columns, slices = 1024 / columns;
+    if (threadIdx.x == 0) s_n = 0;
+    __syncthreads();
+    int n = 0;
+    for (int c = threadIdx.x; c < a.per_group; c += 1024) n += a.part_n[group * a.per_group + c];
+    if (n) atomicAdd(&s_n, n);
+    float t = 0.f;
+    int count = 0;
+    if (col < E)
+#pragma unroll 4
+        for (int c = slice; c < a.per_group; c += slices) {
+            const int64_t at = ((int64_t)group * a.per_group + c) * E + col;
+            count += a.part_c[at];
+            if (a.loss) t += a.part_p[at];
+        }
+    s_p[threadIdx.x] = t;
+    s_c[threadIdx.x] = count;
+    __syncthreads();
+    float term = 0.f;
+    if (slice == 0 && col < E) {
+        for (int k = 1; k < slices; ++k) { t += s_p[k * columns + col]; count += s_c[k * columns + col]; }
+        a.counts[(int64_t)group * E + col] = count;
+        term = (float)count * t;
+    }
+    if (threadIdx.x == 0) a.group_valid[group] = s_n;
+    if (a.loss) {
+        const float sum = workgroup_sum(term, s_sum);
+        if (threadIdx.x == 0) (a.groups == 1 ? a.loss : a.terms + group)[0] = sum * group_scale(a, s_n);
+    }
+}
+
+// loss = sum of the groups' parts (none: 0)
+__global__ __launch_bounds__(1024) void balance_loss_kernel(const float *terms, int groups, float *loss)
+{
+    __shared__ float s[16];
+    float t = 0.f;
+    for (int g = threadIdx.x; g < groups; g += 1024) t += terms[g];
+    const float sum = workgroup_sum(t, s);
+    if (threadIdx.x == 0) loss[0] = sum;
+}
+
+template <class L, int LANES, int V>
+__global__ __launch_bounds__(256) void balance_backward_kernel(BalanceLaunch a)
+{
+    constexpr int SUBS = 256 / LANES;
+    const int E = a.experts, lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+    int group, begin, end;
+    chunk_range(a, blockIdx.x, group, begin, end);
+    int c[V], total = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        c[v] = lane + v * LANES < E ? a.counts[(int64_t)group * E + lane + v * LANES] : 0;
+        total += c[v];
+    }
+#pragma unroll
+    for (int d = LANES / 2; d >= 1; d >>= 1) total += __shfl_xor(total, d, 64);
+    // experts times the distance from the mean, a whole number
+    float dist[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) dist[v] = (float)((int64_t)c[v] * E - total);
+    const float scale = group_scale(a, a.group_valid[group]) / (float)E * (a.dloss ? a.dloss[0] : 1.0f);
+    const L *logits = static_cast<const L *>(a.logits);
+    L *dlogits = static_cast<L *>(a.dlogits);
+    for (int64_t t = begin + sub; t < end; t += SUBS) {
+        if (a.valid && !a.valid[t]) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (lane + v * LANES < E) put(dlogits + t * a.ld + lane + v * LANES, 0.f);
+            continue;
+        }
+        float x[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = lane + v * LANES < E ? logit(logits + t * a.ld + lane + v * LANES) : -INFINITY;
+        softmax<LANES, V>(x);
+        float mean = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) mean = fmaf(x[v], dist[v], mean);
+#pragma unroll
+        for (int d = LANES / 2; d >= 1; d >>= 1) mean += __shfl_xor(mean, d, 64);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (lane + v * LANES < E) put(dlogits + t * a.ld + lane + v * LANES, scale * x[v] * (dist[v] - mean));
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------- host
+int checked(const ficco_expert_balance_t *op, ficco_expert_balance_t *out)
+{
+    if (!op) return FICCO_ERR_ARG;
+    ficco_expert_balance_t o = *op;
+    if (o.logits_type < FICCO_BF16 || o.logits_type > FICCO_F32 || !std::isfinite(o.coefficient)) return FICCO_ERR_ARG;
+    if (o.tokens < 0 || o.tokens > 0x7FFFFFFF || o.experts < 1 || o.experts > 1024 || o.top_k < 1 || o.top_k > 64 || o.group_tokens < 0) return FICCO_ERR_SHAPE;
+    if (!o.group_tokens || o.group_tokens > o.tokens) o.group_tokens = std::max<int64_t>(o.tokens, 1);
+    if ((o.tokens + o.group_tokens - 1) / o.group_tokens > (1 << 20)) return FICCO_ERR_SHAPE;
+    if (!o.ld_logits) o.ld_logits = o.experts;
+    if (o.ld_logits < o.experts || o.ld_logits > kMaxK) return FICCO_ERR_SHAPE;
+    *out = o;
+    return FICCO_OK;
+}
+
+int lanes_of(int experts) { return experts <= 8 ? 8 : experts <= 16 ? 16 : experts <= 32 ? 32 : 64; }
+
+struct Chunks {
+    int64_t groups, per_group, tokens;
+};
+// Chunks for about four workgroups a CU of 256 CUs; a group whose tokens a workgroup takes in 16 turns or fewer is one chunk,
+// which spares the launches that join them.
+Chunks chunks_of(const ficco_expert_balance_t &o)
+{
+    Chunks c{};
+    c.groups = (o.tokens + o.group_tokens - 1) / o.group_tokens;
+    const int64_t turn = 256 / lanes_of(o.experts);
+    const int64_t each = std::max((o.tokens + 1023) / 1024, turn);
+    c.per_group = o.group_tokens <= 16 * turn ? 1 : (o.group_tokens + each - 1) / each;
+    c.tokens = (o.group_tokens + c.per_group - 1) / c.per_group;
+    return c;
+}
+
+struct Workspace {
+    int64_t p, c, n, terms, bytes;
+};
+Workspace workspace_of(const ficco_expert_balance_t &o)
+{
+    const Chunks c = chunks_of(o);
+    Workspace w{};
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += round_up(bytes, 256);
+        return here;
+    };
+    if (c.per_group > 1) {
+        w.p = take(c.groups * c.per_group * o.experts * 4);
+        w.c = take(c.groups * c.per_group * o.experts * 4);
+        w.n = take(c.groups * c.per_group * 4);
+    }
+    if (c.groups > 1) w.terms = take(c.groups * 4);
+    w.bytes = at;
+    return w;
+}
+
+BalanceLaunch launch_of(const ficco_expert_balance_t &o, const Chunks &c)
+{
+    BalanceLaunch a{};
+    a.ld = o.ld_logits;
+    a.tokens = (int32_t)o.tokens;
+    a.group_tokens = (int32_t)o.group_tokens;
+    a.groups = (int32_t)c.groups;
+    a.experts = o.experts;
+    a.top_k = o.top_k;
+    a.per_group = (int32_t)c.per_group;
+    a.chunk_tokens = (int32_t)c.tokens;
+    a.coefficient = o.coefficient;
+    return a;
+}
+
+template <class L, int LANES, int V>
+int launch_t(const BalanceLaunch &a, bool backward, hipStream_t s)
+{
+    const dim3 grid((unsigned)(a.groups * a.per_group)), block(256);
+    if (backward) hipLaunchKernelGGL((balance_backward_kernel<L, LANES, V>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((balance_kernel<L, LANES, V>), grid, block, (256 * V + a.experts) * 4, s, a);
+    HIP_TRY(hipGetLastError());
+    return FICCO_OK;
+}
+template <class L>
+int launch(const BalanceLaunch &a, bool backward, hipStream_t s)
+{
+    if (a.experts <= 8) return launch_t<L, 8, 1>(a, backward, s);
+    if (a.experts <= 16) return launch_t<L, 16, 1>(a, backward, s);
+    if (a.experts <= 32) return launch_t<L, 32, 1>(a, backward, s);
+    if (a.experts <= 64) return launch_t<L, 64, 1>(a, backward, s);
+    if (a.experts <= 128) return launch_t<L, 64, 2>(a, backward, s);
+    if (a.experts <= 256) return launch_t<L, 64, 4>(a, backward, s);
+    if (a.experts <= 512) return launch_t<L, 64, 8>(a, backward, s);
+    return launch_t<L, 64, 16>(a, backward, s);
+}
+
+int forward(const ficco_expert_balance_t *op, const void *logits, const void *ids, const void *valid, void *counts, void *group_valid, void *loss,
+            void *workspace, int64_t workspace_bytes, hipStream_t s)
+{
+    ficco_expert_balance_t o;
+    int rc = checked(op, &o);
+    if (rc) return rc;
+    const bool none = o.tokens == 0;
+    rc = check_args({{logits, o.logits_type == FICCO_F32 ? 4 : 2, none || !loss}, {ids, 4, none}, {valid, 1, true}, {counts, 4, none}, {group_valid, 4, none},
+                     {loss, 4, true}, {workspace, 16, true}});
+    if (rc) return rc;
+    if (none) {
+        if (!loss) return FICCO_OK;
+        hipLaunchKernelGGL(balance_loss_kernel, dim3(1), dim3(1024), 0, s, nullptr, 0, (float *)loss);
+        HIP_TRY(hipGetLastError());
+        return FICCO_OK;
+    }
+    const Chunks c = chunks_of(o);
+    const Workspace w = workspace_of(o);
+    if (w.bytes > 0 && (!workspace || workspace_bytes < w.bytes)) return FICCO_ERR_ARG;
+    unsigned char *const ws = (unsigned char *)workspace;
+    BalanceLaunch a = launch_of(o, c);
+    a.logits = logits;
+    a.ids = (const int32_t *)ids;
+    a.valid = (const uint8_t *)valid;
+    a.counts = (int32_t *)counts;
+    a.group_valid = (int32_t *)group_valid;
+    a.loss = (float *)loss;
+    a.part_p = (float *)(ws + w.p);
+    a.part_c = (int32_t *)(ws + w.c);
+    a.part_n = (int32_t *)(ws + w.n);
+    a.terms = (float *)(ws + w.terms);
+    rc = o.logits_type == FICCO_F32 ? launch<float>(a, false, s) : launch<uint16_t>(a, false, s);
+    if (rc) return rc;
+    if (c.per_group > 1) {
+        int columns = 8;
+        while (columns < o.experts) columns *= 2;
+        hipLaunchKernelGGL(balance_group_kernel, dim3((unsigned)c.groups), dim3(1024), 0, s, a, columns);
+        HIP_TRY(hipGetLastError());
+    }
+    if (loss && c.groups > 1) {
+        hipLaunchKernelGGL(balance_loss_kernel, dim3(1), dim3(1024), 0, s, a.terms, (int)c.groups, (float *)loss);
+        HIP_TRY(hipGetLastError());
+    }
+    return FICCO_OK;
+}
+
+int backward(const ficco_expert_balance_t *op, const void *logits, const void *valid, const void *counts, const void *group_valid, const void *dloss,
+             void *dlogits, hipStream_t s)
+{
+    ficco_expert_balance_t o;
+    int rc = checked(op, &o);
+    if (rc) return rc;
+    const bool none = o.tokens == 0;
+    const int align = o.logits_type == FICCO_F32 ? 4 : 2;
+    rc = check_args({{logits, align, none}, {valid, 1, true}, {counts, 4, none}, {group_valid, 4, none}, {dloss, 4, true}, {dlogits, align, none}});
+    if (rc || none) return rc;
+    BalanceLaunch a = launch_of(o, chunks_of(o));
+    a.logits = logits;
+    a.valid = (const uint8_t *)valid;
+    a.counts = (int32_t *)const_cast<void *>(counts);
+    a.group_valid = (int32_t *)const_cast<void *>(group_valid);
+    a.dloss = (const float *)dloss;
+    a.dlogits = dlogits;
+    return o.logits_type == FICCO_F32 ? launch<float>(a, true, s) : launch<uint16_t>(a, true, s);
+}
+
+}  // namespace
+}  // namespace ficco
+
+using namespace ficco;
+
+extern "C" {
+
+int ficco_expert_balance_workspace(const ficco_expert_balance_t *op, int64_t *bytes)
+{
+    return guarded([&] {
+        ficco_expert_balance_t o;
+        if (!bytes) return (int)FICCO_ERR_ARG;
+        const int rc = checked(op, &o);
+        if (rc) return rc;
+        *bytes = o.tokens ? workspace_of(o).bytes : 0;
+        return (int)FICCO_OK;
+    });
+}
+
+int ficco_expert_balance(const ficco_expert_balance_t *op, const void *logits, const void *ids, const void *valid, void *counts, void *group_valid,
+                         void *loss, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    return guarded([&] { return forward(op, logits, ids, valid, counts, group_valid, loss, workspace, workspace_bytes, (hipStream_t)stream); });
+}
+
+int ficco_expert_balance_backward(const ficco_expert_balance_t *op, const void *logits, const void *valid, const void *counts, const void *group_valid,
+                                  const void *dloss, void *dlogits, void *stream)
+{
+    return guarded([&] { return backward(op, logits, valid, counts, group_valid, dloss, dlogits, (hipStream_t)stream); });
+}
+
+}  // extern "C"

@@ -15,8 +15,7 @@
 // bytes a stage (16 x 32 tiles, twice the CUs, 9.7: half of a weight line is drawn as a whole one), nor reads a stage ahead
 // in a second register buffer (11.1), nor wavefronts of their own for the loads (10.2), nor idle CUs that pull the XCD's
 // lines into its L2 a few stages ahead (no change) made it faster.
-#include "ficco_internal.h"
-#include "ficco_mfma.h"
+#include "ficco_epilogue.h"
 
 namespace ficco {
 namespace {
@@ -47,8 +46,18 @@ struct DirectCfg {
 
 static __device__ __forceinline__ int w_swizzle(int row) { return 2 * (((row >> 1) & 1) | (((row >> 3) & 1) << 1)); }
 
-template <class T>
-__global__ __launch_bounds__(T::THREADS) void gemm_direct_kernel(DirectLaunch a)
+// What a launch has beside its operands: nothing, or the linear operator's epilogue and row strides.
+struct Bare {
+    static constexpr bool ON = false;
+};
+struct WithEpilogue {
+    static constexpr bool ON = true;
+    Epilogue e;
+    int64_t lda, ldc;
+};
+
+template <class T, class Extra>
+__global__ __launch_bounds__(T::THREADS) void gemm_direct_kernel(DirectLaunch a, Extra extra)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const int lane = threadIdx.x & 63;
@@ -62,7 +71,9 @@ __global__ __launch_bounds__(T::THREADS) void gemm_direct_kernel(DirectLaunch a)
     const int KS = (K + T::BK - 1) / T::BK;
     const bool half_tail = (K & 64) != 0;              // the last stage has one half only
 
-    const uint16_t *const A = scalar_base(a.A + (int64_t)row0 * K);
+    int lda = K;
+    if constexpr (Extra::ON) lda = scalar((int)extra.lda);
+    const uint16_t *const A = scalar_base(a.A + (int64_t)row0 * lda);
     const uint16_t *const W = scalar_base(a.W + col0);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
 
@@ -75,7 +86,7 @@ __global__ __launch_bounds__(T::THREADS) void gemm_direct_kernel(DirectLaunch a)
         const int b = i * 4 + wave;
         const int row = b % (2 * T::FM) * 8 + lane / 8;
         half_a[i] = b / (2 * T::FM);
-        off_a[i] = (uint32_t)(min(row, rows_valid - 1) * K + ((lane % 8) ^ ((row >> 1) & 7)) * 8) * 2u;
+        off_a[i] = (uint32_t)(min(row, rows_valid - 1) * lda + ((lane % 8) ^ ((row >> 1) & 7)) * 8) * 2u;
     }
     // W: rows i * 32 + wave * 8 ... + 7 of a half; slots past the last column read the last one
     const int w_slot = min((lane % 8) ^ w_swizzle(wave * 8 + lane / 8), cols_valid / 8 - 1);
@@ -183,6 +194,19 @@ __global__ __launch_bounds__(T::THREADS) void gemm_direct_kernel(DirectLaunch a)
 
     // acc[i][v] is C[16 i + lane % 16][16 wave + 4 (lane / 16) + v]; N and with it cols_valid are multiples of 8
     const int n = 16 * wave + 4 * g;
+    if constexpr (Extra::ON) {
+        if (n < cols_valid) {
+            const f32x4_t bias = bias4(extra.e, col0 + n);
+            with_activation(extra.e.activation, [&](auto act) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < T::FM; ++i) {
+                    const int64_t m = row0 + 16 * i + j;
+                    if (16 * i + j < rows_valid) store4<act.value>(extra.e, acc[i], bias, a.C + m * extra.ldc + col0 + n, m, col0 + n);
+                }
+            });
+        }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < T::FM; ++i) {
         const int m = 16 * i + j;
@@ -196,30 +220,39 @@ typedef DirectCfg<1, 7> D16;
 typedef DirectCfg<2, 6> D32;
 typedef DirectCfg<4, 4> D64;
 
-template <class T>
-hipError_t launch_direct_t(const DirectLaunch &a, hipStream_t s)
+template <class T, class Extra>
+hipError_t launch_direct_t(const DirectLaunch &a, const Extra &extra, hipStream_t s)
 {
-    static hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(&gemm_direct_kernel<T>),
+    static hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(&gemm_direct_kernel<T, Extra>),
                                                  hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES);
     if (once != hipSuccess) return once;
     DirectLaunch b = a;
     b.tiles_m = (a.M + T::BM - 1) / T::BM;
     b.tiles_n = (a.N + T::BN - 1) / T::BN;
-    hipLaunchKernelGGL(gemm_direct_kernel<T>, dim3((unsigned)(b.tiles_m * b.tiles_n)), dim3(T::THREADS), T::LDS_BYTES, s, b);
+    hipLaunchKernelGGL((gemm_direct_kernel<T, Extra>), dim3((unsigned)(b.tiles_m * b.tiles_n)), dim3(T::THREADS), T::LDS_BYTES, s, b, extra);
     return hipGetLastError();
+}
+
+template <class Extra>
+hipError_t launch_direct_of(int row_blocks, const DirectLaunch &a, const Extra &extra, hipStream_t s)
+{
+    if (a.M < 1 || a.N < 8 || a.N % 8 || a.K < kBK || a.K % kBK || a.K > kMaxK || (int64_t)a.K * a.N * 2 > 0x7FFFFFFF) return hipErrorInvalidValue;
+    switch (row_blocks) {
+    case 1: return launch_direct_t<D16>(a, extra, s);
+    case 2: return launch_direct_t<D32>(a, extra, s);
+    case 4: return launch_direct_t<D64>(a, extra, s);
+    default: return hipErrorInvalidValue;
+    }
 }
 
 }  // namespace
 
-hipError_t launch_direct(int row_blocks, const DirectLaunch &a, hipStream_t s)
+hipError_t launch_direct(int row_blocks, const DirectLaunch &a, hipStream_t s) { return launch_direct_of(row_blocks, a, Bare{}, s); }
+
+hipError_t launch_direct_epilogue(int row_blocks, const DirectLaunch &a, const Epilogue &e, int64_t lda, int64_t ldc, hipStream_t s)
 {
-    if (a.M < 1 || a.N < 8 || a.N % 8 || a.K < kBK || a.K % kBK || a.K > kMaxK || (int64_t)a.K * a.N * 2 > 0x7FFFFFFF) return hipErrorInvalidValue;
-    switch (row_blocks) {
-    case 1: return launch_direct_t<D16>(a, s);
-    case 2: return launch_direct_t<D32>(a, s);
-    case 4: return launch_direct_t<D64>(a, s);
-    default: return hipErrorInvalidValue;
-    }
+    if (lda < a.K || lda > kMaxK || ldc < a.N) return hipErrorInvalidValue;
+    return launch_direct_of(row_blocks, a, WithEpilogue{e, lda, ldc}, s);
 }
 
 }  // namespace ficco

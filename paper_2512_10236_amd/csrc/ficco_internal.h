@@ -360,6 +360,9 @@ struct DirectLaunch {
     int32_t tiles_m, tiles_n;     // set by the launcher
 };
 hipError_t launch_direct(int row_blocks, const DirectLaunch &a, hipStream_t s);
+// The same with the linear operator's epilogue (ficco_epilogue.h) and with rows of A and C at strides of their own.
+struct Epilogue;
+hipError_t launch_direct_epilogue(int row_blocks, const DirectLaunch &a, const Epilogue &e, int64_t lda, int64_t ldc, hipStream_t s);
 // W[K,N] -> Wt[N,K]; also clears up to 256 words at `clear`
 hipError_t launch_pack_weight(const uint16_t *W, uint16_t *Wt, int64_t K, int64_t N, hipStream_t s, uint32_t *clear = nullptr, int clear_words = 0);
 int resident_grid_size(int tile, int device);

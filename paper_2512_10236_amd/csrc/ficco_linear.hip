@@ -1,0 +1,450 @@
+// A product with bias, activation and residual in its epilogue, and its gradients (ficco_linear, ficco_linear_backward):
+//   z = A W + b,  C = act(z) + R          dZ = dC act'(z),  db = sum_m dZ,  dA = dZ W^T,  dW = A^T dZ
+// The products run on the tile routine of the GEMM kernels (ficco_tile.h): both operands with k contiguous, bf16 in, fp32
+// accumulators, k ascending. The epilogue takes the accumulators before they are rounded, so that bias, activation and
+// residual cost no pass over memory of their own.
+//
+// The backward pass is bound by its two products. What they need beside their inputs is made once by turn_kernel, a streaming
+// kernel: dZ (with its column sums), and the operands with the other index contiguous.
+#include "ficco_operators.h"
+#include "ficco_epilogue.h"
+
+namespace ficco {
+namespace {
+
+struct LinearLaunch {
+    const uint16_t *A, *Wt;       // [M,K] stride lda, [N,K] dense
+    uint16_t *C;
+    int64_t lda, ldc;
+    int32_t M, N, K, group_m;
+    Epilogue e;
+};
+
+// One launch over all tiles, at most as many workgroups as run at once; the tiles in the order of gemm_blocks_kernel.
+template <class T>
+__global__ __launch_bounds__(T::THREADS) void linear_tiles_kernel(LinearLaunch a)
+{
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const int tiles_n = (a.N + T::BN - 1) / T::BN;
+    const int tiles_m = (int)(((int64_t)a.M + T::BM - 1) / T::BM);
+    const XcdRun run = xcd_run(blockIdx.x, gridDim.x, tiles_m * tiles_n);
+    const int per_group = a.group_m * tiles_n;
+    for (int t = run.first; t < run.count; t += run.stride) {
+        const int lid = run.start + t;
+        const int group = lid / per_group;
+        const int first_m = group * a.group_m;
+        const int gsz = min(tiles_m - first_m, a.group_m);
+        const int tm = first_m + (lid % per_group) % gsz;
+        const int tn = (lid % per_group) / gsz;
+        const int64_t row0 = (int64_t)tm * T::BM;
+        const int rows_valid = (int)min((int64_t)T::BM, a.M - row0);
+        const int col0 = tn * T::BN;
+        const int cols_valid = min(T::BN, a.N - col0);
+        TileAcc<T> ta;
+        tile_zero(ta);
+        tile_accumulate<T>(ta, a.A + row0 * a.lda, rows_valid, a.Wt + (int64_t)col0 * a.K, cols_valid, a.lda, a.K, a.K, smem);
+        with_activation(a.e.activation, [&](auto act) __attribute__((always_inline)) {
+            tile_store_epilogue<T, act.value>(ta, a.e, a.C + row0 * a.ldc + col0, rows_valid, cols_valid, a.ldc, row0, col0);
+        });
+        __syncthreads();                   // everyone is done with the ring before the next tile refills it
+    }
+    wait_vmem<0>();                        // no load may arrive in LDS that is not this workgroup's any more
+}
+
+template <class T>
+int launch_tiles_t(const LinearLaunch &a, hipStream_t s)
+{
+    const int64_t tiles_n = ((int64_t)a.N + T::BN - 1) / T::BN, tiles_m = ((int64_t)a.M + T::BM - 1) / T::BM, total = tiles_m * tiles_n;
+    if (total <= 0 || total > 0x7FFFFFFF || a.lda > kMaxK || a.K > kMaxK) return FICCO_ERR_SHAPE;
+    static int fit_of[64];                 // per device: workgroups that run at once, 0 = not asked yet
+    int dev = 0;
+    HIP_TRY(hipGetDevice(&dev));
+    int fit = dev < 64 ? fit_of[dev] : 0;
+    if (fit == 0) {
+        int per_cu = 0;
+        HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(&linear_tiles_kernel<T>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES));
+        HIP_TRY(hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, linear_tiles_kernel<T>, T::THREADS, T::LDS_BYTES));
+        fit = std::max(8, per_cu * compute_units() / 8 * 8);
+        if (dev < 64) fit_of[dev] = fit;
+    }
+    const int64_t grid = std::min<int64_t>(total, fit);
+    LinearLaunch b = a;
+    b.group_m = 8;
+    if (total > grid) {
+        double best = -1;
+        for (int g = 1; g <= 8; g *= 2) {
+            const double c = tile_order_cost(T::BM, T::BN, tiles_n, tiles_m, grid / 8, 1, g, (int64_t)a.M * a.K * 2, (int64_t)a.N * a.K * 2);
+            if (best < 0 || c < best) { best = c; b.group_m = g; }
+        }
+    }
+    hipLaunchKernelGGL(linear_tiles_kernel<T>, dim3((unsigned)grid), dim3(T::THREADS), T::LDS_BYTES, s, b);
+    HIP_TRY(hipGetLastError());
+    return FICCO_OK;
+}
+
+int launch_tiles(int tile, const LinearLaunch &a, hipStream_t s)
+{
+    switch (tile) {
+#define X(id, T) case id: return launch_tiles_t<T>(a, s);
+    FICCO_FOR_EACH_TILE(X)
+#undef X
+    default: return FICCO_ERR_ARG;
+    }
+}
+
+// The tile rule's answer for one launch over an M x K x N product with its operands in place.
+int tile_for(int64_t M, int64_t K, int64_t N, double *us)
+{
+    ficco_plan_t shape;
+    shape.M = M; shape.K = K; shape.N = N; shape.G = 1; shape.c = 1;
+    shape.schedule = FICCO_SERIAL;
+    shape.order = FICCO_ORDER_STEP_MAJOR;
+    shape.mode = FICCO_MODE_GEMM_ONLY;
+    if (build_lists(&shape)) return 0;
+    return choose_tile(&shape, compute_units(), false, us);
+}
+
+// ---------------------------------------------------------------------------------------------- turned operands, dZ
+// src [R][Cc] (stride ld), 64 x 64 values a wavefront: a lane holds 8 rows x 8 columns, loads 16 bytes of each of 8 rows, turns
+// the block with byte permutes and stores 16 bytes of each of 8 columns, so that loads and stores are whole 128-byte lines.
+//   turned  [Cc][ldt], ldt = R rounded up to 64: src transposed, zero behind its end (null: not wanted)
+//   with z (stride ldz): the value is src * act'(z), rounded to bf16, instead of src
+//   same    [R][lds], lds = Cc rounded up to 64: the value in its own order, zero behind its end (null: not wanted)
+//   sums    [ceil(R/256)][Cc] fp32: column sums over 256 rows each, of the values before they are rounded (null: not wanted)
+// Streaming, bound by memory.
+struct TurnLaunch {
+    const uint16_t *src, *z;
+    uint16_t *turned, *same;
+    float *sums;
+    int64_t R, Cc, ld, ldz, ldt, lds;
+};
+constexpr int kTurnRows = 256;
+
+template <int ACT>
+__global__ __launch_bounds__(256) void turn_kernel(TurnLaunch a)
+{
+    __shared__ float s_sum[4][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t r0 = (int64_t)blockIdx.y * kTurnRows + wave * 64 + (lane & 7) * 8;
+    const int64_t c0 = (int64_t)blockIdx.x * 64 + (lane >> 3) * 8;
+    u32x4_t v[8];
+    float sum[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) sum[c] = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        v[i] = u32x4_t{0u, 0u, 0u, 0u};
+        if (r0 + i < a.R && c0 < a.Cc) v[i] = *reinterpret_cast<const u32x4_t *>(a.src + (r0 + i) * a.ld + c0);
+    }
+    if constexpr (ACT != FICCO_ACT_NONE) {
+        u32x4_t zz[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            zz[i] = u32x4_t{0u, 0u, 0u, 0u};
+            if (r0 + i < a.R && c0 < a.Cc) zz[i] = *reinterpret_cast<const u32x4_t *>(a.z + (r0 + i) * a.ldz + c0);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int p = 0; p < 4; ++p) {
+                const float lo = bf16_lo(v[i][p]) * slope<ACT>(bf16_lo(zz[i][p])), hi = bf16_hi(v[i][p]) * slope<ACT>(bf16_hi(zz[i][p]));
+                const bool there = r0 + i < a.R && c0 < a.Cc;
+                sum[2 * p] += there ? lo : 0.f;
+                sum[2 * p + 1] += there ? hi : 0.f;
+                v[i][p] = there ? pack2_bf16_rne(lo, hi) : 0u;
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int p = 0; p < 4; ++p) { sum[2 * p] += bf16_lo(v[i][p]); sum[2 * p + 1] += bf16_hi(v[i][p]); }
+    }
+    if (a.same) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (r0 + i < a.R && c0 < a.lds) *reinterpret_cast<u32x4_t *>(a.same + (r0 + i) * a.lds + c0) = v[i];
+    }
+    if (a.turned && r0 < a.ldt && c0 < a.Cc) {
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+            u32x4_t even, odd;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                even[i] = __builtin_amdgcn_perm(v[2 * i + 1][p], v[2 * i][p], 0x05040100u);
+                odd[i] = __builtin_amdgcn_perm(v[2 * i + 1][p], v[2 * i][p], 0x07060302u);
+            }
+            *reinterpret_cast<u32x4_t *>(a.turned + (c0 + 2 * p) * a.ldt + r0) = even;
+            *reinterpret_cast<u32x4_t *>(a.turned + (c0 + 2 * p + 1) * a.ldt + r0) = odd;
+        }
+    }
+    if (a.sums) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+            for (int m = 1; m < 8; m <<= 1) sum[c] += __shfl_xor(sum[c], m, 64);
+        if ((lane & 7) == 0)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) s_sum[wave][(lane >> 3) * 8 + c] = sum[c];
+        __syncthreads();
+        const int64_t c = (int64_t)blockIdx.x * 64 + threadIdx.x;
+        if (threadIdx.x < 64 && c < a.Cc)
+            a.sums[(int64_t)blockIdx.y * a.Cc + c] = (s_sum[0][threadIdx.x] + s_sum[1][threadIdx.x]) + (s_sum[2][threadIdx.x] + s_sum[3][threadIdx.x]);
+    }
+}
+
+int launch_turn(int activation, const TurnLaunch &a, hipStream_t s)
+{
+    if (a.R < 1 || a.Cc < 8 || a.Cc % 8) return FICCO_ERR_SHAPE;
+    const dim3 grid((unsigned)((a.Cc + 63) / 64), (unsigned)((a.R + kTurnRows - 1) / kTurnRows)), block(256);
+    switch (activation) {
+    case FICCO_ACT_NONE: hipLaunchKernelGGL(turn_kernel<FICCO_ACT_NONE>, grid, block, 0, s, a); break;
+    case FICCO_ACT_RELU: hipLaunchKernelGGL(turn_kernel<FICCO_ACT_RELU>, grid, block, 0, s, a); break;
+    case FICCO_ACT_GELU: hipLaunchKernelGGL(turn_kernel<FICCO_ACT_GELU>, grid, block, 0, s, a); break;
+    case FICCO_ACT_GELU_TANH: hipLaunchKernelGGL(turn_kernel<FICCO_ACT_GELU_TANH>, grid, block, 0, s, a); break;
+    case FICCO_ACT_SILU: hipLaunchKernelGGL(turn_kernel<FICCO_ACT_SILU>, grid, block, 0, s, a); break;
+    default: return FICCO_ERR_ARG;
+    }
+    HIP_TRY(hipGetLastError());
+    return FICCO_OK;
+}
+
+// out[c] = sum over r of in[r][c], r in [0, R): 64 columns a workgroup, its 16 wavefronts take every 16th row. R = 0: zeros.
+__global__ __launch_bounds__(1024) void sum_rows_kernel(const float *__restrict__ in, float *__restrict__ out, int R, int64_t Cc)
+{
+    __shared__ float s[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
+    float t = 0.f;
+    if (c < Cc)
+#pragma unroll 4
+        for (int r = wave; r < R; r += 16) t += in[(int64_t)r * Cc + c];
+    s[wave][lane] = t;
+    __syncthreads();
+    if (wave == 0 && c < Cc) {
+#pragma unroll
+        for (int w = 1; w < 16; ++w) t += s[w][lane];
+        out[c] = t;
+    }
+}
+
+__global__ __launch_bounds__(256) void zero_kernel(u32x4_t *p, int64_t vecs)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < vecs; i += (int64_t)gridDim.x * 256) p[i] = u32x4_t{0u, 0u, 0u, 0u};
+}
+
+// ------------------------------------------------------------------------------------------------------------- host
+// The struct with its defaults filled in; an error where it breaks a rule.
+int checked(const ficco_linear_t *op, bool backward, ficco_linear_t *out)
+{
+    if (!op) return FICCO_ERR_ARG;
+    ficco_linear_t o = *op;
+    if (o.weight_layout < FICCO_WEIGHT_KN || o.weight_layout > FICCO_WEIGHT_NK || o.activation < FICCO_ACT_NONE || o.activation > FICCO_ACT_SILU ||
+        o.bias_type < FICCO_BF16 || o.bias_type > FICCO_F32 || o.reserved)
+        return FICCO_ERR_ARG;
+    if (o.M < 0 || o.M > (backward ? kMaxK : 0x7FFFFFFF) || o.K < 1 || o.K % 64 || o.K > kMaxK || o.N < 1 || o.N % 8 || o.N > kMaxK) return FICCO_ERR_SHAPE;
+    if (!o.lda) o.lda = o.K;
+    if (!o.ldc) o.ldc = o.N;
+    if (!o.ld_residual) o.ld_residual = o.N;
+    if (!o.ld_pre) o.ld_pre = o.N;
+    if (o.lda < o.K || o.lda % 8 || o.lda > kMaxK || o.ldc < o.N || o.ldc % 8 || o.ldc > kMaxK || o.ld_residual < o.N || o.ld_residual % 8 || o.ld_pre < o.N ||
+        o.ld_pre % 8)
+        return FICCO_ERR_SHAPE;
+    *out = o;
+    return FICCO_OK;
+}
+
+// How a forward goes: row blocks of the direct kernel, which takes the [K,N] weight as it is, or 0 and the tile of the others.
+struct Forward {
+    int row_blocks, tile;
+    int64_t bytes;
+};
+Forward forward_way(const ficco_linear_t &o)
+{
+    Forward f{0, 0, 0};
+    if (o.M == 0) return f;
+    double us = 0;
+    f.tile = tile_for(o.M, o.K, o.N, &us);
+    if (o.weight_layout == FICCO_WEIGHT_KN) {
+        if (o.K * o.N * 2 <= 0x7FFFFFFF) f.row_blocks = direct_row_blocks(o.M, o.K, o.N, compute_units(), us);
+        if (!f.row_blocks) f.bytes = round_up(o.K * o.N * 2, 256);
+    }
+    return f;
+}
+
+// The backward's workspace, in bytes from its start (-1: not needed).
+struct Backward {
+    int64_t Mp, Np;               // M and N rounded up to whole k-tiles
+    int64_t dz, dz_turned, a_turned, w_other, sums, bytes;
+};
+Backward backward_way(const ficco_linear_t &o)
+{
+    Backward b{};
+    b.Mp = round_up(o.M, kBK);
+    b.Np = round_up(o.N, kBK);
+    if (o.M == 0) return b;
+    int64_t at = 0;
+    auto take = [&](bool needed, int64_t bytes) {
+        const int64_t here = at;
+        if (needed) at += round_up(bytes, 256);
+        return needed ? here : -1;
+    };
+    b.dz = take(o.activation != FICCO_ACT_NONE || b.Np != o.N, o.M * b.Np * 2);
+    b.dz_turned = take(true, o.N * b.Mp * 2);
+    b.a_turned = take(true, o.K * b.Mp * 2);
+    b.w_other = take(o.weight_layout == FICCO_WEIGHT_NK || b.Np != o.N, o.K * b.Np * 2);
+    b.sums = take(true, (o.M + kTurnRows - 1) / kTurnRows * o.N * 4);
+    b.bytes = at;
+    return b;
+}
+
+// C[M,N] = A[M,K] B[N,K]^T with both operands k-contiguous and K a multiple of the k-tile.
+int product(int64_t M, int64_t K, int64_t N, const uint16_t *A, int64_t lda, const uint16_t *B, uint16_t *C, hipStream_t s)
+{
+    GemmLaunch g{};
+    g.A = A;
+    g.Wt = B;
+    g.C = C;
+    g.lda = lda;
+    g.ldc = N;
+    g.N = (int32_t)N;
+    g.K = (int32_t)K;
+    g.n_blocks = 1;
+    g.rows_per_block = (int32_t)M;
+    HIP_TRY(launch_gemm(tile_for(M, K, N, nullptr), g, s));
+    return FICCO_OK;
+}
+
+int zero(void *p, int64_t bytes, hipStream_t s)
+{
+    hipLaunchKernelGGL(zero_kernel, dim3((unsigned)std::min<int64_t>((bytes / 16 + 255) / 256, 1024)), dim3(256), 0, s, (u32x4_t *)p, bytes / 16);
+    HIP_TRY(hipGetLastError());
+    return FICCO_OK;
+}
+
+int sum_rows(const float *in, float *out, int64_t R, int64_t Cc, hipStream_t s)
+{
+    hipLaunchKernelGGL(sum_rows_kernel, dim3((unsigned)((Cc + 63) / 64)), dim3(1024), 0, s, in, out, (int)R, Cc);
+    HIP_TRY(hipGetLastError());
+    return FICCO_OK;
+}
+
+int forward(const ficco_linear_t *op, const void *A, const void *W, const void *bias, const void *residual, void *pre, void *C, void *workspace,
+            int64_t workspace_bytes, hipStream_t s)
+{
+    ficco_linear_t o;
+    int rc = checked(op, false, &o);
+    if (rc) return rc;
+    const bool none = o.M == 0;
+    rc = check_args({{A, 16, none}, {W, 16, none}, {bias, o.bias_type == FICCO_F32 ? 4 : 2, true}, {residual, 16, true}, {pre, 16, true}, {C, 16, none}, {workspace, 16, true}});
+    if (rc || none) return rc;
+    const Forward f = forward_way(o);
+    if (f.bytes > 0 && (!workspace || workspace_bytes < f.bytes)) return FICCO_ERR_ARG;
+    Epilogue e{bias, (const uint16_t *)residual, (uint16_t *)pre, o.ld_residual, o.ld_pre, o.activation, o.bias_type == FICCO_F32};
+    if (f.row_blocks) {
+        DirectLaunch d{};
+        d.A = (const uint16_t *)A;
+        d.W = (const uint16_t *)W;
+        d.C = (uint16_t *)C;
+        d.M = (int32_t)o.M; d.N = (int32_t)o.N; d.K = (int32_t)o.K;
+        HIP_TRY(launch_direct_epilogue(f.row_blocks, d, e, o.lda, o.ldc, s));
+        return FICCO_OK;
+    }
+    const uint16_t *wt = (const uint16_t *)W;
+    if (o.weight_layout == FICCO_WEIGHT_KN) {
+        HIP_TRY(launch_pack_weight((const uint16_t *)W, (uint16_t *)workspace, o.K, o.N, s));
+        wt = (const uint16_t *)workspace;
+    }
+    const LinearLaunch a{(const uint16_t *)A, wt, (uint16_t *)C, o.lda, o.ldc, (int32_t)o.M, (int32_t)o.N, (int32_t)o.K, 0, e};
+    return launch_tiles(f.tile, a, s);
+}
+
+int backward(const ficco_linear_t *op, const void *A, const void *W, const void *pre, const void *dC, void *dA, void *dW, void *dbias, void *workspace,
+             int64_t workspace_bytes, hipStream_t s)
+{
+    ficco_linear_t o;
+    int rc = checked(op, true, &o);
+    if (rc) return rc;
+    const bool none = o.M == 0, act = o.activation != FICCO_ACT_NONE;
+    rc = check_args({{A, 16, none || !dW}, {W, 16, none || !dA}, {pre, 16, none || !act}, {dC, 16, none}, {dA, 16, true}, {dW, 16, true}, {dbias, 4, true},
+                     {workspace, 16, none}});
+    if (rc) return rc;
+    const int64_t M = o.M, K = o.K, N = o.N;
+    if (none) {
+        if (dW && (rc = zero(dW, K * N * 2, s))) return rc;
+        return dbias ? sum_rows(nullptr, (float *)dbias, 0, N, s) : FICCO_OK;
+    }
+    const Backward b = backward_way(o);
+    if (workspace_bytes < b.bytes) return FICCO_ERR_ARG;
+    if (!dA && !dW && !dbias) return FICCO_OK;
+    unsigned char *const ws = (unsigned char *)workspace;
+    auto at = [&](int64_t off) { return off < 0 ? nullptr : (uint16_t *)(ws + off); };
+    const bool kn = o.weight_layout == FICCO_WEIGHT_KN;
+
+    TurnLaunch t{};
+    t.src = (const uint16_t *)dC;
+    t.z = (const uint16_t *)pre;
+    t.turned = dW ? at(b.dz_turned) : nullptr;
+    t.same = dA ? at(b.dz) : nullptr;
+    t.sums = dbias ? (float *)at(b.sums) : nullptr;
+    t.R = M; t.Cc = N; t.ld = o.ldc; t.ldz = o.ld_pre; t.ldt = b.Mp; t.lds = b.Np;
+    if (t.turned || t.same || t.sums)
+        if ((rc = launch_turn(o.activation, t, s))) return rc;
+    if (dbias && (rc = sum_rows((const float *)at(b.sums), (float *)dbias, (M + kTurnRows - 1) / kTurnRows, N, s))) return rc;
+    if (dA) {
+        // both operands with n contiguous: dZ, and W as [K,N]
+        const uint16_t *w = (const uint16_t *)W;
+        if (b.w_other >= 0) {
+            TurnLaunch u{};
+            u.src = (const uint16_t *)W;
+            if (kn) { u.R = K; u.Cc = N; u.ld = N; u.same = at(b.w_other); u.lds = b.Np; u.ldt = round_up(K, kBK); }
+            else { u.R = N; u.Cc = K; u.ld = K; u.turned = at(b.w_other); u.ldt = b.Np; u.lds = K; }
+            if ((rc = launch_turn(FICCO_ACT_NONE, u, s))) return rc;
+            w = at(b.w_other);
+        }
+        const bool own = b.dz >= 0;
+        if ((rc = product(M, b.Np, K, own ? at(b.dz) : (const uint16_t *)dC, own ? b.Np : o.ldc, w, (uint16_t *)dA, s))) return rc;
+    }
+    if (dW) {
+        // both operands with m contiguous, in the order that gives dW W's layout
+        TurnLaunch u{};
+        u.src = (const uint16_t *)A;
+        u.R = M; u.Cc = K; u.ld = o.lda; u.turned = at(b.a_turned); u.ldt = b.Mp; u.lds = K;
+        if ((rc = launch_turn(FICCO_ACT_NONE, u, s))) return rc;
+        const uint16_t *first = at(kn ? b.a_turned : b.dz_turned), *second = at(kn ? b.dz_turned : b.a_turned);
+        if ((rc = product(kn ? K : N, b.Mp, kn ? N : K, first, b.Mp, second, (uint16_t *)dW, s))) return rc;
+    }
+    return FICCO_OK;
+}
+
+}  // namespace
+}  // namespace ficco
+
+using namespace ficco;
+
+extern "C" {
+
+int ficco_linear_workspace(const ficco_linear_t *op, int backward, int64_t *bytes)
+{
+    return guarded([&] {
+        ficco_linear_t o;
+        if (!bytes) return (int)FICCO_ERR_ARG;
+        const int rc = checked(op, backward != 0, &o);
+        if (rc) return rc;
+        *bytes = backward ? backward_way(o).bytes : forward_way(o).bytes;
+        return (int)FICCO_OK;
+    });
+}
+
+int ficco_linear(const ficco_linear_t *op, const void *A, const void *W, const void *bias, const void *residual, void *pre, void *C, void *workspace,
+                 int64_t workspace_bytes, void *stream)
+{
+    return guarded([&] { return forward(op, A, W, bias, residual, pre, C, workspace, workspace_bytes, (hipStream_t)stream); });
+}
+
+int ficco_linear_backward(const ficco_linear_t *op, const void *A, const void *W, const void *pre, const void *dC, void *dA, void *dW, void *dbias,
+                          void *workspace, int64_t workspace_bytes, void *stream)
+{
+    return guarded([&] { return backward(op, A, W, pre, dC, dA, dW, dbias, workspace, workspace_bytes, (hipStream_t)stream); });
+}
+
+}  // extern "C"

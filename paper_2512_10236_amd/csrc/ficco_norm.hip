@@ -1,0 +1,528 @@
+// What stands between two blocks of a layer (ficco_residual_norm and its backward): norm behind a block, gate, scaled residual
+// stream, norm in front of the next block. With D = width, r(v) = 1 / sqrt(mean(v^2) + eps):
+//   n = p b r(b),  y = s x + g n,  h = w y r(y)
+//   u = w dh,      dY = dy + r(y) (u - y r(y)^2 mean(u y)),  dx = s dY
+//   dn = g dY,     db = r(b) (p dn - b r(b)^2 mean(p dn b)),  dg = sum dY n,  dp = sum dn b r(b),  dw = sum dh y r(y)
+//
+// Streaming work, bound by memory: a row lives in the registers of the threads that own it (V vectors of 8 values each)
+// between its loads and its stores, and is read once. All sums are fp32.
+#include "ficco_operators.h"
+#include "ficco_epilogue.h"
+
+namespace ficco {
+namespace {
+
+struct NormLaunch {
+    const void *x;                // forward: x; backward: y
+    const uint16_t *block;
+    const void *post, *gate, *pre;
+    void *y;                      // forward: y; backward: dx
+    uint16_t *h;                  // forward: h; backward: dblock
+    const void *dy;
+    const uint16_t *dh;
+    float *sums;                  // backward: [3][chunks][width] partial sums of dpost, dgate, dpre
+    float *dgate;                 // backward: rows of dgate that a chunk holds whole groups of, else null
+    int32_t rows, width, gate_rows, param_f32;
+    int32_t chunks, per_group, chunk_rows;     // backward: chunk c is the (c % per_group)-th run of chunk_rows rows of its group, ...
+    int32_t want_post, want_gate, want_pre;    // ... or, with per_group 0, of all rows
+    float scale, eps;
+};
+
+struct Vec8 {
+    float f[8];
+};
+static __device__ __forceinline__ Vec8 widen(u32x4_t v)
+{
+    Vec8 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { o.f[2 * i] = bf16_lo(v[i]); o.f[2 * i + 1] = bf16_hi(v[i]); }
+    return o;
+}
+static __device__ __forceinline__ u32x4_t narrow(const Vec8 &v)
+{
+    return u32x4_t{pack2_bf16_rne(v.f[0], v.f[1]), pack2_bf16_rne(v.f[2], v.f[3]), pack2_bf16_rne(v.f[4], v.f[5]), pack2_bf16_rne(v.f[6], v.f[7])};
+}
+static __device__ __forceinline__ Vec8 from_f32(const float *p)
+{
+    Vec8 o;
+    const f32x4_t a = reinterpret_cast<const f32x4_t *>(p)[0], b = reinterpret_cast<const f32x4_t *>(p)[1];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { o.f[i] = a[i]; o.f[4 + i] = b[i]; }
+    return o;
+}
+// 8 values from element `at` (a multiple of 8) on, of either type
+template <bool F32>
+static __device__ __forceinline__ Vec8 load8(const void *p, int64_t at)
+{
+    if constexpr (F32) return from_f32(static_cast<const float *>(p) + at);
+    else return widen(*reinterpret_cast<const u32x4_t *>(static_cast<const uint16_t *>(p) + at));
+}
+static __device__ __forceinline__ Vec8 param8(const void *p, int f32, int64_t at) { return f32 ? load8<true>(p, at) : load8<false>(p, at); }
+template <bool F32>
+static __device__ __forceinline__ void store8(void *p, int64_t at, const Vec8 &v)
+{
+    if constexpr (F32) {
+        f32x4_t *o = reinterpret_cast<f32x4_t *>(static_cast<float *>(p) + at);
+        o[0] = f32x4_t{v.f[0], v.f[1], v.f[2], v.f[3]};
+        o[1] = f32x4_t{v.f[4], v.f[5], v.f[6], v.f[7]};
+    } else {
+        *reinterpret_cast<u32x4_t *>(static_cast<uint16_t *>(p) + at) = narrow(v);
+    }
+}
+
+// Sums of N values over the TPR threads of a row; every thread gets them. `s`: N floats for each of the row's wavefronts, not
+// in use by an earlier call that a wavefront may still read.
+template <int TPR, int N>
+static __device__ __forceinline__ void row_sum(float (&v)[N], float *s)
+{
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1)
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], m, 64);
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int k = 0; k < N; ++k) s[(threadIdx.x >> 6) * N + k] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            float t = 0.f;
+#pragma unroll
+            for (int w = 0; w < TPR / 64; ++w) t += s[w * N + k];
+            v[k] = t;
+        }
+    }
+}
+
+// TPR threads a row (a wavefront, with four rows a workgroup, or a whole workgroup), V vectors of 8 values a thread.
+template <int TPR, int V>
+struct RowCfg {
+    static constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
+};
+
+template <int TPR, int V, bool F32>
+__global__ __launch_bounds__((RowCfg<TPR, V>::THREADS)) void residual_norm_kernel(NormLaunch a)
+{
+    constexpr int ROWS = RowCfg<TPR, V>::ROWS;
+    __shared__ float s_post[TPR / 64], s_pre[TPR / 64];
+    const int lane = threadIdx.x % TPR;
+    const float inv = 1.0f / (float)a.width;
+    const int vecs = a.width / 8;
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * ROWS) {
+        const int64_t at = row * a.width;
+        const int64_t gate_at = a.gate && a.gate_rows ? (int64_t)((int)row / a.gate_rows) * a.width : 0;
+        u32x4_t b[V];
+        Vec8 y[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int i = lane + v * TPR;
+            b[v] = u32x4_t{0u, 0u, 0u, 0u};
+            if (i < vecs) b[v] = *reinterpret_cast<const u32x4_t *>(a.block + at + i * 8);
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int i = lane + v * TPR;
+            y[v] = Vec8{};
+            if (i < vecs) y[v] = load8<F32>(a.x, at + i * 8);
+        }
+        float r = 1.0f;
+        if (a.post) {
+            float ss[1] = {0.f};
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const Vec8 w = widen(b[v]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ss[0] = fmaf(w.f[e], w.f[e], ss[0]);
+            }
+            row_sum<TPR, 1>(ss, s_post);
+            r = rsqrtf(fmaf(ss[0], inv, a.eps));
+        }
+        float ss[1] = {0.f};
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int i = lane + v * TPR;
+            if (i < vecs) {
+                Vec8 n = widen(b[v]);
+                if (a.post) {
+                    const Vec8 p = param8(a.post, a.param_f32, i * 8);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) n.f[e] *= r * p.f[e];
+                }
+                if (a.gate) {
+                    const Vec8 g = param8(a.gate, a.param_f32, gate_at + i * 8);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) n.f[e] *= g.f[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    y[v].f[e] = fmaf(a.scale, y[v].f[e], n.f[e]);
+                    ss[0] = fmaf(y[v].f[e], y[v].f[e], ss[0]);
+                }
+                store8<F32>(a.y, at + i * 8, y[v]);
+            }
+        }
+        if (a.h) {
+            row_sum<TPR, 1>(ss, s_pre);
+            r = rsqrtf(fmaf(ss[0], inv, a.eps));
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int i = lane + v * TPR;
+                if (i < vecs) {
+                    const Vec8 w = param8(a.pre, a.param_f32, i * 8);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[v].f[e] *= r * w.f[e];
+                    store8<false>(a.h, at + i * 8, y[v]);
+                }
+            }
+        }
+        if constexpr (TPR > 64) __syncthreads();       // the sums' places are used again
+    }
+}
+
+// The backward's rows go in chunks, each walked by one group of TPR threads, which keeps its columns' partial sums in registers
+// and writes them once: sums over rows in a fixed order, without atomics.
+template <int TPR, int V, bool F32>
+__global__ __launch_bounds__((RowCfg<TPR, V>::THREADS)) void residual_norm_backward_kernel(NormLaunch a)
+{
+    constexpr int ROWS = RowCfg<TPR, V>::ROWS;
+    __shared__ float s_a[3 * (TPR / 64)], s_b[TPR / 64];
+    const int lane = threadIdx.x % TPR, chunk = blockIdx.x * ROWS + threadIdx.x / TPR;
+    if (TPR == 64 && chunk >= a.chunks) return;
+    const float inv = 1.0f / (float)a.width;
+    const int vecs = a.width / 8;
+    int64_t begin = (int64_t)chunk * a.chunk_rows, end = begin + a.chunk_rows;
+    if (a.per_group) {
+        const int g = chunk / a.per_group;
+        begin = (int64_t)g * a.gate_rows + (int64_t)(chunk % a.per_group) * a.chunk_rows;
+        end = min(begin + a.chunk_rows, (int64_t)(g + 1) * a.gate_rows);
+    }
+    end = min(end, (int64_t)a.rows);
+    Vec8 dpost[V], dgate[V], dpre[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) dpost[v] = dgate[v] = dpre[v] = Vec8{};
+    for (int64_t row = begin; row < end; ++row) {
+        const int64_t at = row * a.width;
+        const int group = a.gate_rows ? (int)row / a.gate_rows : 0;
+        const int64_t gate_at = (int64_t)group * a.width;
+        Vec8 d[V], y[V], b[V], dh[V];      // d: dy, then dY, then post * dn
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int i = lane + v * TPR;
+            d[v] = y[v] = b[v] = dh[v] = Vec8{};
+            if (i < vecs) {
+                if (a.dy) d[v] = load8<F32>(a.dy, at + i * 8);
+                if (a.dh) { y[v] = load8<F32>(a.x, at + i * 8); dh[v] = load8<false>(a.dh, at + i * 8); }
+                if (a.block) b[v] = load8<false>(a.block, at + i * 8);
+            }
+        }
+        float s[3] = {0.f, 0.f, 0.f};      // y^2, u y, b^2
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int i = lane + v * TPR;
+            if (i < vecs) {
+                if (a.dh) {
+                    const Vec8 w = param8(a.pre, a.param_f32, i * 8);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        s[0] = fmaf(y[v].f[e], y[v].f[e], s[0]);
+                        s[1] = fmaf(w.f[e] * dh[v].f[e], y[v].f[e], s[1]);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[2] = fmaf(b[v].f[e], b[v].f[e], s[2]);
+            }
+        }
+        row_sum<TPR, 3>(s, s_a);
+        const float r = rsqrtf(fmaf(s[0], inv, a.eps)), back = r * r * r * s[1] * inv;
+        const float rb = a.post ? rsqrtf(fmaf(s[2], inv, a.eps)) : 1.0f;
+        float s4[1] = {0.f};
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int i = lane + v * TPR;
+            if (i < vecs) {
+                if (a.dh) {
+                    const Vec8 w = param8(a.pre, a.param_f32, i * 8);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        d[v].f[e] += fmaf(r * w.f[e], dh[v].f[e], -y[v].f[e] * back);
+                        dpre[v].f[e] = fmaf(dh[v].f[e] * r, y[v].f[e], dpre[v].f[e]);
+                    }
+                }
+                if (a.y) {
+                    Vec8 o;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) o.f[e] = a.scale * d[v].f[e];
+                    store8<F32>(a.y, at + i * 8, o);
+                }
+                Vec8 p = Vec8{};
+                if (a.post) p = param8(a.post, a.param_f32, i * 8);
+                if (a.gate) {
+                    const Vec8 g = param8(a.gate, a.param_f32, gate_at + i * 8);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float n = a.post ? b[v].f[e] * rb * p.f[e] : b[v].f[e];
+                        dgate[v].f[e] = fmaf(d[v].f[e], n, dgate[v].f[e]);
+                        d[v].f[e] *= g.f[e];
+                    }
+                }
+                if (a.post) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        dpost[v].f[e] = fmaf(d[v].f[e], b[v].f[e] * rb, dpost[v].f[e]);
+                        d[v].f[e] *= p.f[e];
+                        s4[0] = fmaf(d[v].f[e], b[v].f[e], s4[0]);
+                    }
+                }
+            }
+        }
+        if (a.post) row_sum<TPR, 1>(s4, s_b);
+        if (a.h) {
+            const float back_b = rb * rb * rb * s4[0] * inv;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int i = lane + v * TPR;
+                if (i < vecs) {
+                    if (a.post)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) d[v].f[e] = fmaf(rb, d[v].f[e], -b[v].f[e] * back_b);
+                    store8<false>(a.h, at + i * 8, d[v]);
+                }
+            }
+        }
+        // a group of rows that share a gate ends inside the chunk: it lies in it whole
+        if (a.dgate && (row + 1 == end || (int)(row + 1) / a.gate_rows != group)) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int i = lane + v * TPR;
+                if (i < vecs) store8<true>(a.dgate, gate_at + i * 8, dgate[v]);
+                dgate[v] = Vec8{};
+            }
+        }
+        if constexpr (TPR > 64) __syncthreads();       // the sums' places are used again
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int i = lane + v * TPR;
+        if (i < vecs) {
+            const int64_t plane = (int64_t)a.chunks * a.width, at = (int64_t)chunk * a.width + i * 8;
+            if (a.want_post) store8<true>(a.sums, at, dpost[v]);
+            if (a.want_gate && !a.dgate) store8<true>(a.sums, plane + at, dgate[v]);
+            if (a.want_pre) store8<true>(a.sums, 2 * plane + at, dpre[v]);
+        }
+    }
+}
+
+// Sums of the chunks' partial sums, 64 columns a workgroup, 16 wavefronts taking every 16th chunk. blockIdx.y = 0: dpost over all
+// chunks, 1: dpre, 2 + g: dgate of group g over its own chunks.
+struct SumLaunch {
+    const float *sums;
+    float *dpost, *dgate, *dpre;
+    int32_t chunks, per_group, width;
+};
+__global__ __launch_bounds__(1024) void residual_norm_sum_kernel(SumLaunch a)
+{
+    __shared__ float s[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+    const int64_t plane = (int64_t)a.chunks * a.width;
+    const int y = blockIdx.y;
+    const float *in = y == 0 ? a.sums : y == 1 ? a.sums + 2 * plane : a.sums + plane + (int64_t)(y - 2) * a.per_group * a.width;
+    float *out = y == 0 ? a.dpost : y == 1 ? a.dpre : a.dgate ? a.dgate + (int64_t)(y - 2) * a.width : nullptr;
+    if (!out) return;
+    const int n = y < 2 ? a.chunks : a.per_group;
+    float t = 0.f;
+    if (c < a.width)
+#pragma unroll 8
+        for (int k = wave; k < n; k += 16) t += in[(int64_t)k * a.width + c];
+    s[wave][lane] = t;
+    __syncthreads();
+    if (wave == 0 && c < a.width) {
+#pragma unroll
+        for (int w = 1; w < 16; ++w) t += s[w][lane];
+        out[c] = t;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------------- host
+int checked(const ficco_residual_norm_t *op, ficco_residual_norm_t *out)
+{
+    if (!op) return FICCO_ERR_ARG;
+    const ficco_residual_norm_t &o = *op;
+    if (o.stream_type < FICCO_BF16 || o.stream_type > FICCO_F32 || o.param_type < FICCO_BF16 || o.param_type > FICCO_F32) return FICCO_ERR_ARG;
+    if (!(o.eps >= 0.f) || !std::isfinite(o.eps) || !std::isfinite(o.residual_scale)) return FICCO_ERR_ARG;
+    if (o.rows < 0 || o.rows > 0x7FFFFFFF || o.width < 8 || o.width % 8 || o.width > 16384 || o.gate_rows < 0) return FICCO_ERR_SHAPE;
+    *out = o;
+    if (out->gate_rows > std::max<int64_t>(o.rows, 1)) out->gate_rows = std::max<int64_t>(o.rows, 1);
+    return FICCO_OK;
+}
+
+// Threads a row in the backward: what its three partial sums and four operands leave room for, V = 1 or 2 vectors a thread.
+int backward_tpr(int64_t width) { return width <= 1024 ? 64 : width <= 4096 ? 256 : width <= 8192 ? 512 : 1024; }
+
+struct Chunks {
+    int64_t chunks, per_group, rows, groups;
+    bool whole_groups;            // a chunk holds whole groups: it writes their dgate itself
+};
+Chunks chunks_of(const ficco_residual_norm_t &o)
+{
+    // two workgroups a CU of 256 CUs
+    const int64_t target = std::max<int64_t>(256, 131072 / backward_tpr(o.width));
+    const int64_t each = std::max<int64_t>(1, (o.rows + target - 1) / target);
+    Chunks c{};
+    if (!o.gate_rows || o.gate_rows >= o.rows) {
+        c.groups = 1;
+        c.rows = each;
+        c.chunks = c.per_group = (o.rows + each - 1) / each;
+    } else if (o.gate_rows >= each) {
+        c.groups = (o.rows + o.gate_rows - 1) / o.gate_rows;
+        c.per_group = (o.gate_rows + each - 1) / each;
+        c.rows = (o.gate_rows + c.per_group - 1) / c.per_group;
+        c.chunks = c.groups * c.per_group;
+    } else {
+        c.whole_groups = true;
+        c.rows = each / o.gate_rows * o.gate_rows;
+        c.chunks = (o.rows + c.rows - 1) / c.rows;
+    }
+    return c;
+}
+int64_t workspace_of(const ficco_residual_norm_t &o) { return o.rows ? 3 * chunks_of(o).chunks * o.width * 4 : 0; }
+
+template <int TPR, int V>
+int launch_forward_t(const NormLaunch &a, bool f32, hipStream_t s)
+{
+    typedef RowCfg<TPR, V> R;
+    const dim3 grid((unsigned)std::min<int64_t>(((int64_t)a.rows + R::ROWS - 1) / R::ROWS, 1 << 20)), block(R::THREADS);
+    if (f32) hipLaunchKernelGGL((residual_norm_kernel<TPR, V, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((residual_norm_kernel<TPR, V, false>), grid, block, 0, s, a);
+    HIP_TRY(hipGetLastError());
+    return FICCO_OK;
+}
+
+int launch_forward(const NormLaunch &a, bool f32, hipStream_t s)
+{
+    if (a.width <= 512) return launch_forward_t<64, 1>(a, f32, s);
+    if (a.width <= 1024) return launch_forward_t<64, 2>(a, f32, s);
+    if (a.width <= 2048) return launch_forward_t<256, 1>(a, f32, s);
+    if (a.width <= 4096) return launch_forward_t<256, 2>(a, f32, s);
+    if (a.width <= 8192) return launch_forward_t<256, 4>(a, f32, s);
+    return launch_forward_t<512, 4>(a, f32, s);
+}
+
+template <int TPR, int V>
+int launch_backward_t(const NormLaunch &a, bool f32, hipStream_t s)
+{
+    typedef RowCfg<TPR, V> R;
+    const dim3 grid((unsigned)((a.chunks + R::ROWS - 1) / R::ROWS)), block(R::THREADS);
+    if (f32) hipLaunchKernelGGL((residual_norm_backward_kernel<TPR, V, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((residual_norm_backward_kernel<TPR, V, false>), grid, block, 0, s, a);
+    HIP_TRY(hipGetLastError());
+    return FICCO_OK;
+}
+
+int launch_backward(const NormLaunch &a, bool f32, hipStream_t s)
+{
+    const int tpr = backward_tpr(a.width), v = (a.width / 8 + tpr - 1) / tpr;
+    if (v == 1) {
+        if (tpr == 64) return launch_backward_t<64, 1>(a, f32, s);
+        if (tpr == 256) return launch_backward_t<256, 1>(a, f32, s);
+    } else if (v == 2) {
+        if (tpr == 64) return launch_backward_t<64, 2>(a, f32, s);
+        if (tpr == 256) return launch_backward_t<256, 2>(a, f32, s);
+        if (tpr == 512) return launch_backward_t<512, 2>(a, f32, s);
+        if (tpr == 1024) return launch_backward_t<1024, 2>(a, f32, s);
+    }
+    return FICCO_ERR_SHAPE;
+}
+
+int forward(const ficco_residual_norm_t *op, const void *x, const void *block, const void *post, const void *gate, const void *pre, void *y, void *h,
+            hipStream_t s)
+{
+    ficco_residual_norm_t o;
+    int rc = checked(op, &o);
+    if (rc) return rc;
+    const bool none = o.rows == 0;
+    if (!pre != !h) return FICCO_ERR_ARG;
+    rc = check_args({{x, 16, none}, {block, 16, none}, {post, 16, true}, {gate, 16, true}, {pre, 16, true}, {y, 16, none}, {h, 16, true}});
+    if (rc || none) return rc;
+    NormLaunch a{};
+    a.x = x; a.block = (const uint16_t *)block; a.post = post; a.gate = gate; a.pre = pre; a.y = y; a.h = (uint16_t *)h;
+    a.rows = (int32_t)o.rows; a.width = (int32_t)o.width; a.gate_rows = (int32_t)o.gate_rows;
+    a.param_f32 = o.param_type == FICCO_F32;
+    a.scale = o.residual_scale; a.eps = o.eps;
+    return launch_forward(a, o.stream_type == FICCO_F32, s);
+}
+
+int backward(const ficco_residual_norm_t *op, const void *y, const void *block, const void *post, const void *gate, const void *pre, const void *dy,
+             const void *dh, void *dx, void *dblock, void *dpost, void *dgate, void *dpre, void *workspace, int64_t workspace_bytes, hipStream_t s)
+{
+    ficco_residual_norm_t o;
+    int rc = checked(op, &o);
+    if (rc) return rc;
+    const bool none = o.rows == 0, sums = dpost || dgate || dpre;
+    if ((dpost && !post) || (dgate && !gate) || (dpre && !pre) || (dpre && !dh && !none) || (dh && !pre)) return FICCO_ERR_ARG;
+    const bool needs_block = post || dgate;
+    rc = check_args({{y, 16, none || !dh}, {block, 16, none || !needs_block}, {post, 16, true}, {gate, 16, true}, {pre, 16, true}, {dy, 16, true}, {dh, 16, true},
+                     {dx, 16, true}, {dblock, 16, true}, {dpost, 16, true}, {dgate, 16, true}, {dpre, 16, true}, {workspace, 16, none || !sums}});
+    if (rc) return rc;
+    if (sums && workspace_bytes < workspace_of(o)) return FICCO_ERR_ARG;
+    if (!dx && !dblock && !sums) return FICCO_OK;
+    const Chunks c = chunks_of(o);
+    SumLaunch t{(const float *)workspace, (float *)dpost, nullptr, (float *)dpre, (int32_t)c.chunks, (int32_t)c.per_group, (int32_t)o.width};
+    int groups = 0;
+    if (dgate && !c.whole_groups && (!none || !op->gate_rows)) { t.dgate = (float *)dgate; groups = (int)c.groups; }
+    if (!none) {
+        NormLaunch a{};
+        a.x = y; a.block = needs_block ? (const uint16_t *)block : nullptr; a.post = post; a.gate = gate; a.pre = pre;
+        a.y = dx; a.h = (uint16_t *)dblock; a.dy = dy; a.dh = (const uint16_t *)dh;
+        a.sums = (float *)workspace;
+        a.dgate = c.whole_groups ? (float *)dgate : nullptr;
+        a.rows = (int32_t)o.rows; a.width = (int32_t)o.width; a.gate_rows = (int32_t)o.gate_rows;
+        a.param_f32 = o.param_type == FICCO_F32;
+        a.chunks = (int32_t)c.chunks; a.chunk_rows = (int32_t)c.rows;
+        a.per_group = c.groups > 1 ? (int32_t)c.per_group : 0;
+        a.want_post = dpost != nullptr; a.want_gate = dgate != nullptr; a.want_pre = dpre != nullptr;
+        a.scale = o.residual_scale; a.eps = o.eps;
+        if ((rc = launch_backward(a, o.stream_type == FICCO_F32, s))) return rc;
+    }
+    if (dpost || dpre || t.dgate) {
+        hipLaunchKernelGGL(residual_norm_sum_kernel, dim3((unsigned)((o.width + 63) / 64), (unsigned)(2 + groups)), dim3(1024), 0, s, t);
+        HIP_TRY(hipGetLastError());
+    }
+    return FICCO_OK;
+}
+
+}  // namespace
+}  // namespace ficco
+
+using namespace ficco;
+
+extern "C" {
+
+int ficco_residual_norm_workspace(const ficco_residual_norm_t *op, int64_t *bytes)
+{
+    return guarded([&] {
+        ficco_residual_norm_t o;
+        if (!bytes) return (int)FICCO_ERR_ARG;
+        const int rc = checked(op, &o);
+        if (rc) return rc;
+        *bytes = workspace_of(o);
+        return (int)FICCO_OK;
+    });
+}
+
+int ficco_residual_norm(const ficco_residual_norm_t *op, const void *x, const void *block, const void *post_weight, const void *gate,
+                        const void *pre_weight, void *y, void *h, void *stream)
+{
+    return guarded([&] { return forward(op, x, block, post_weight, gate, pre_weight, y, h, (hipStream_t)stream); });
+}
+
+int ficco_residual_norm_backward(const ficco_residual_norm_t *op, const void *y, const void *block, const void *post_weight, const void *gate,
+                                 const void *pre_weight, const void *dy, const void *dh, void *dx, void *dblock, void *dpost_weight, void *dgate,
+                                 void *dpre_weight, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    return guarded([&] {
+        return backward(op, y, block, post_weight, gate, pre_weight, dy, dh, dx, dblock, dpost_weight, dgate, dpre_weight, workspace, workspace_bytes,
+                        (hipStream_t)stream);
+    });
+}
+
+}  // extern "C"
