@@ -570,7 +570,7 @@ typedef enum ficco_weight_layout {
  * each of dA, dW, dbias NULL if it is not wanted; the residual's gradient is dC. dZ is rounded to bf16 for the two products
  * (they are bf16 products) and not for dbias. act' of FICCO_ACT_RELU at 0 is 0.
  * Row strides in elements, 0 = dense: lda of A, ldc of C and of dC, ld_residual, ld_pre; multiples of 8, at least the row's
- * length, lda and ldc at most 2^22. Shape rules (FICCO_ERR_SHAPE): 0 <= M < 2^31, K % 64 == 0, N % 8 == 0, K and N
+ * length and at most 2^22. Shape rules (FICCO_ERR_SHAPE): 0 <= M < 2^31, K % 64 == 0, N % 8 == 0, K and N
  * positive and at most 2^22; the backward pass needs M <= 2^22. With M == 0 nothing is read; dW and dbias are zero.
  * Workspace: the forward of a [K,N] weight keeps its re-laid out copy there (K N 2 bytes) unless the product is small; the
  * backward keeps dZ and the operands that its products need with another order of their values.

@@ -364,15 +364,17 @@ def ficco_ideal_overlap_us(t_comm_us, t_gemm_us, n):
 def _addr(x):
     """Address of a buffer, a tensor or a stream, or None. A tensor's strides are the caller's to describe in `op`: one whose
     last dimension is not contiguous cannot be."""
-    if x is None or isinstance(x, int):
-        return x
-    if hasattr(x, "data_ptr"):
-        if x.dim() and x.stride(-1) != 1 and x.size(-1) > 1:
-            raise FiccoError(FICCO_ERR_ARG, "a tensor's last dimension must be contiguous")
-        return x.data_ptr()
-    if hasattr(x, "cuda_stream"):
+    if x is None:
+        return None
+    try:
+        p = x.data_ptr()
+    except AttributeError:
+        if isinstance(x, int):
+            return x
         return x.cuda_stream
-    raise TypeError(type(x))
+    if not x.is_contiguous() and x.stride(-1) != 1 and x.size(-1) > 1:
+        raise FiccoError(FICCO_ERR_ARG, "a tensor's last dimension must be contiguous")
+    return p
 
 
 def ficco_linear_workspace(op, backward=False):

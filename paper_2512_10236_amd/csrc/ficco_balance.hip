@@ -7,6 +7,7 @@
 // next to its parts where a router is nearly even, so it is taken of the counts' distances from their mean, which are exact.
 #include "ficco_operators.h"
 #include "ficco_epilogue.h"
+#include "ficco_lanes.h"
 
 namespace ficco {
 namespace {
@@ -22,7 +23,8 @@ struct BalanceLaunch {
     // partial results of a chunk of tokens, where a group has several: [chunks][E], [chunks][E], [chunks]
     float *part_p;
     int32_t *part_c, *part_n;
-    float *terms;                 // [groups] the groups' parts of the loss
+    float *terms;                 // [n_terms] parts of the loss: of the groups, or of 64 experts of a group each (one: the loss itself)
+    int32_t n_terms;
     int64_t ld;
     int32_t tokens, group_tokens, groups, experts, top_k;
     int32_t per_group, chunk_tokens;       // chunk c: the (c % per_group)-th run of chunk_tokens tokens of group c / per_group
@@ -33,6 +35,53 @@ static __device__ __forceinline__ float logit(const float *p) { return *p; }
 static __device__ __forceinline__ float logit(const uint16_t *p) { return __uint_as_float((uint32_t)*p << 16); }
 static __device__ __forceinline__ void put(float *p, float v) { *p = v; }
 static __device__ __forceinline__ void put(uint16_t *p, float v) { *p = (uint16_t)pack2_bf16_rne(v, 0.f); }
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+static __device__ __forceinline__ f32x4_t logit4(const float *p) { return *reinterpret_cast<const f32x4_t *>(p); }
+static __device__ __forceinline__ f32x4_t logit4(const uint16_t *p)
+{
+    const u32x2_t v = *reinterpret_cast<const u32x2_t *>(p);
+    return f32x4_t{bf16_lo(v[0]), bf16_hi(v[0]), bf16_lo(v[1]), bf16_hi(v[1])};
+}
+static __device__ __forceinline__ void put4(float *p, f32x4_t v) { *reinterpret_cast<f32x4_t *>(p) = v; }
+static __device__ __forceinline__ void put4(uint16_t *p, f32x4_t v) { *reinterpret_cast<u32x2_t *>(p) = u32x2_t{pack2_bf16_rne(v[0], v[1]), pack2_bf16_rne(v[2], v[3])}; }
+
+// A token's logits over LANES lanes, V each. Lane l has the experts l, l + LANES, ...; or, with FOURS (V a multiple of 4, rows of
+// whole fours and aligned to them), the fours l, l + LANES, ...
+template <int LANES, int V, bool FOURS>
+struct Spread {
+    static constexpr int TOKENS = V <= 4 ? 4 : V <= 8 ? 2 : 1;     // tokens that a lane loads before it uses the first
+    static __device__ __forceinline__ int expert(int lane, int v) { return FOURS ? 4 * (lane + v / 4 * LANES) + v % 4 : lane + v * LANES; }
+    template <class L>
+    static __device__ __forceinline__ void load(float (&x)[V], const L *row, int lane, int E)
+    {
+        if constexpr (FOURS) {
+#pragma unroll
+            for (int q = 0; q < V / 4; ++q)
+                if (expert(lane, 4 * q) < E) {
+                    const f32x4_t f = logit4(row + expert(lane, 4 * q));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[4 * q + i] = f[i];
+                }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (expert(lane, v) < E) x[v] = logit(row + expert(lane, v));
+        }
+    }
+    template <class L>
+    static __device__ __forceinline__ void store(const float (&x)[V], L *row, int lane, int E)
+    {
+        if constexpr (FOURS) {
+#pragma unroll
+            for (int q = 0; q < V / 4; ++q)
+                if (expert(lane, 4 * q) < E) put4(row + expert(lane, 4 * q), f32x4_t{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]});
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (expert(lane, v) < E) put(row + expert(lane, v), x[v]);
+        }
+    }
+};
 
 // s of a group with n valid tokens
 static __device__ __forceinline__ float group_scale(const BalanceLaunch &a, int n)
@@ -49,16 +98,14 @@ static __device__ __forceinline__ void chunk_range(const BalanceLaunch &a, int c
     end = (int)max(e, (int64_t)begin);
 }
 
-// The probabilities of a token, in place of its logits: LANES lanes with V logits each, expert lane + v * LANES. A token whose
-// logits are all -inf has none.
+// The probabilities of a token, in place of its logits. A token whose logits are all -inf has none.
 template <int LANES, int V>
 static __device__ __forceinline__ void softmax(float (&x)[V])
 {
     float m = -INFINITY;
 #pragma unroll
     for (int v = 0; v < V; ++v) m = fmaxf(m, x[v]);
-#pragma unroll
-    for (int d = LANES / 2; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+    m = lane_max<LANES>(m);
     if (m == -INFINITY) m = 0.f;
     float s = 0.f;
 #pragma unroll
@@ -66,11 +113,46 @@ static __device__ __forceinline__ void softmax(float (&x)[V])
         x[v] = __builtin_amdgcn_exp2f((x[v] - m) * kLog2E);
         s += x[v];
     }
-#pragma unroll
-    for (int d = LANES / 2; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
+    s = lane_sum<LANES>(s);
     const float r = s == 0.f ? 0.f : 1.0f / s;
 #pragma unroll
     for (int v = 0; v < V; ++v) x[v] *= r;
+}
+
+// Calls f(token, probabilities) for the tokens [begin, end) of a workgroup's share, LANES lanes a token and TOKENS of them at a time, so that their
+// loads are in flight together. Padding, and what is behind the end, has no probabilities; its logits are not read.
+template <class L, int LANES, int V, bool FOURS, class Fn>
+static __device__ __forceinline__ void for_tokens(const BalanceLaunch &a, int begin, int end, Fn &&f)
+{
+    typedef Spread<LANES, V, FOURS> S;
+    constexpr int SUBS = 256 / LANES, T = S::TOKENS;
+    const int lane = threadIdx.x % LANES, sub = LANES == 64 ? scalar(threadIdx.x / 64) : threadIdx.x / LANES;
+    const L *logits = static_cast<const L *>(a.logits);
+    int64_t first = begin + sub;
+    int use[T];
+    auto look = [&](int64_t t0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < T; ++k) {
+            const int64_t t = t0 + k * SUBS;
+            use[k] = t < end;
+            if (a.valid && t < end) use[k] = a.valid[t];
+        }
+    };
+    look(first);
+    for (; first < end; first += T * SUBS) {
+        float x[T][V];
+#pragma unroll
+        for (int k = 0; k < T; ++k) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[k][v] = -INFINITY;
+            if (LANES == 64 ? scalar(use[k]) : use[k]) S::load(x[k], logits + (first + k * SUBS) * a.ld, lane, a.experts);
+        }
+        look(first + T * SUBS);
+#pragma unroll
+        for (int k = 0; k < T; ++k) softmax<LANES, V>(x[k]);
+#pragma unroll
+        for (int k = 0; k < T; ++k) f(first + k * SUBS, x[k]);
+    }
 }
 
 // Sum over a workgroup of 4 wavefronts (256 threads) or 16, in a fixed order; thread 0 has it.
@@ -87,9 +169,10 @@ static __device__ __forceinline__ float workgroup_sum(float v, float *s)
 }
 
 // One chunk of tokens a workgroup. Where a group is one chunk (per_group == 1) it writes the group's results.
-template <class L, int LANES, int V>
+template <class L, int LANES, int V, bool FOURS>
 __global__ __launch_bounds__(256) void balance_kernel(BalanceLaunch a)
 {
+    typedef Spread<LANES, V, FOURS> S;
     constexpr int SUBS = 256 / LANES;
     extern __shared__ float s_p[];         // [SUBS][LANES * V], then the chunk's counts
     __shared__ float s_sum[4];
@@ -110,23 +193,17 @@ __global__ __launch_bounds__(256) void balance_kernel(BalanceLaunch a)
         for (int t = begin + (int)threadIdx.x; t < end; t += 256) n += a.valid[t] != 0;
         if (n) atomicAdd(&s_n, n);
     }
-    const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
     if (a.loss) {
+        const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
         float p[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) p[v] = 0.f;
-        const L *logits = static_cast<const L *>(a.logits);
-        for (int64_t t = begin + sub; t < end; t += SUBS) {
-            if (a.valid && !a.valid[t]) continue;
-            float x[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) x[v] = lane + v * LANES < E ? logit(logits + t * a.ld + lane + v * LANES) : -INFINITY;
-            softmax<LANES, V>(x);
+        for_tokens<L, LANES, V, FOURS>(a, begin, end, [&](int64_t, const float (&x)[V]) __attribute__((always_inline)) {
 #pragma unroll
             for (int v = 0; v < V; ++v) p[v] += x[v];
-        }
+        });
 #pragma unroll
-        for (int v = 0; v < V; ++v) s_p[sub * LANES * V + lane + v * LANES] = p[v];
+        for (int v = 0; v < V; ++v) s_p[sub * LANES * V + S::expert(lane, v)] = p[v];
     }
     __syncthreads();
     const int n = a.valid ? s_n : end - begin;
@@ -147,19 +224,19 @@ __global__ __launch_bounds__(256) void balance_kernel(BalanceLaunch a)
         if (threadIdx.x == 0) a.group_valid[group] = n;
         if (a.loss) {
             const float sum = workgroup_sum(term, s_sum);
-            if (threadIdx.x == 0) (a.groups == 1 ? a.loss : a.terms + group)[0] = sum * group_scale(a, n);
+            if (threadIdx.x == 0) (a.n_terms == 1 ? a.loss : a.terms + group)[0] = sum * group_scale(a, n);
         }
     } else if (threadIdx.x == 0) {
         a.part_n[blockIdx.x] = n;
     }
 }
 
-// The chunks' results of one group, a workgroup each: `columns` (a power of two) threads side by side over the experts.
-__global__ __launch_bounds__(1024) void balance_group_kernel(BalanceLaunch a, int columns)
+// The chunks' results of group blockIdx.x for 64 experts from 64 blockIdx.y on; 16 wavefronts take every 16th chunk.
+__global__ __launch_bounds__(1024) void balance_group_kernel(BalanceLaunch a)
 {
-    __shared__ float s_p[1024], s_sum[16];
-    __shared__ int s_c[1024], s_n;
-    const int E = a.experts, group = blockIdx.x, col = threadIdx.x & (columns - 1), slice = threadIdx.x / columns, slices = 1024 / columns;
+    __shared__ float s_p[16][64];
+    __shared__ int s_c[16][64], s_n;
+    const int E = a.experts, group = blockIdx.x, lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), e = blockIdx.y * 64 + lane;
     if (threadIdx.x == 0) s_n = 0;
     __syncthreads();
     int n = 0;
@@ -167,50 +244,49 @@ __global__ __launch_bounds__(1024) void balance_group_kernel(BalanceLaunch a, in
     if (n) atomicAdd(&s_n, n);
     float t = 0.f;
     int count = 0;
-    if (col < E)
+    if (e < E)
 #pragma unroll 4
-        for (int c = slice; c < a.per_group; c += slices) {
-            const int64_t at = ((int64_t)group * a.per_group + c) * E + col;
+        for (int c = wave; c < a.per_group; c += 16) {
+            const int64_t at = ((int64_t)group * a.per_group + c) * E + e;
             count += a.part_c[at];
             if (a.loss) t += a.part_p[at];
         }
-    s_p[threadIdx.x] = t;
-    s_c[threadIdx.x] = count;
+    s_p[wave][lane] = t;
+    s_c[wave][lane] = count;
     __syncthreads();
-    float term = 0.f;
-    if (slice == 0 && col < E) {
-        for (int k = 1; k < slices; ++k) { t += s_p[k * columns + col]; count += s_c[k * columns + col]; }
-        a.counts[(int64_t)group * E + col] = count;
-        term = (float)count * t;
-    }
-    if (threadIdx.x == 0) a.group_valid[group] = s_n;
+    if (wave) return;
+#pragma unroll
+    for (int k = 1; k < 16; ++k) { t += s_p[k][lane]; count += s_c[k][lane]; }
+    if (e < E) a.counts[(int64_t)group * E + e] = count;
+    if (threadIdx.x == 0 && blockIdx.y == 0) a.group_valid[group] = s_n;
     if (a.loss) {
-        const float sum = workgroup_sum(term, s_sum);
-        if (threadIdx.x == 0) (a.groups == 1 ? a.loss : a.terms + group)[0] = sum * group_scale(a, s_n);
+        const float sum = lane_sum<64>((float)count * t);
+        if (threadIdx.x == 0) (a.n_terms == 1 ? a.loss : a.terms + (int64_t)group * gridDim.y + blockIdx.y)[0] = sum * group_scale(a, s_n);
     }
 }
 
 // loss = sum of the groups' parts (none: 0)
-__global__ __launch_bounds__(1024) void balance_loss_kernel(const float *terms, int groups, float *loss)
+__global__ __launch_bounds__(1024) void balance_loss_kernel(const float *terms, int n, float *loss)
 {
     __shared__ float s[16];
     float t = 0.f;
-    for (int g = threadIdx.x; g < groups; g += 1024) t += terms[g];
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += 1024) t += terms[i];
     const float sum = workgroup_sum(t, s);
     if (threadIdx.x == 0) loss[0] = sum;
 }
 
-template <class L, int LANES, int V>
+template <class L, int LANES, int V, bool FOURS>
 __global__ __launch_bounds__(256) void balance_backward_kernel(BalanceLaunch a)
 {
-    constexpr int SUBS = 256 / LANES;
-    const int E = a.experts, lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
+    typedef Spread<LANES, V, FOURS> S;
+    const int E = a.experts, lane = threadIdx.x % LANES;
     int group, begin, end;
     chunk_range(a, blockIdx.x, group, begin, end);
     int c[V], total = 0;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        c[v] = lane + v * LANES < E ? a.counts[(int64_t)group * E + lane + v * LANES] : 0;
+        c[v] = S::expert(lane, v) < E ? a.counts[(int64_t)group * E + S::expert(lane, v)] : 0;
         total += c[v];
     }
 #pragma unroll
@@ -220,28 +296,16 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(BalanceLaunch a)
 #pragma unroll
     for (int v = 0; v < V; ++v) dist[v] = (float)((int64_t)c[v] * E - total);
     const float scale = group_scale(a, a.group_valid[group]) / (float)E * (a.dloss ? a.dloss[0] : 1.0f);
-    const L *logits = static_cast<const L *>(a.logits);
     L *dlogits = static_cast<L *>(a.dlogits);
-    for (int64_t t = begin + sub; t < end; t += SUBS) {
-        if (a.valid && !a.valid[t]) {
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (lane + v * LANES < E) put(dlogits + t * a.ld + lane + v * LANES, 0.f);
-            continue;
-        }
-        float x[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = lane + v * LANES < E ? logit(logits + t * a.ld + lane + v * LANES) : -INFINITY;
-        softmax<LANES, V>(x);
-        float mean = 0.f;
+    for_tokens<L, LANES, V, FOURS>(a, begin, end, [&](int64_t t, const float (&x)[V]) __attribute__((always_inline)) {
+        float mean = 0.f, d[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) mean = fmaf(x[v], dist[v], mean);
+        mean = lane_sum<LANES>(mean);
 #pragma unroll
-        for (int d = LANES / 2; d >= 1; d >>= 1) mean += __shfl_xor(mean, d, 64);
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (lane + v * LANES < E) put(dlogits + t * a.ld + lane + v * LANES, scale * x[v] * (dist[v] - mean));
-    }
+        for (int v = 0; v < V; ++v) d[v] = scale * x[v] * (dist[v] - mean);
+        if (t < end) S::store(d, dlogits + t * a.ld, lane, E);
+    });
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -278,7 +342,7 @@ Chunks chunks_of(const ficco_expert_balance_t &o)
 }
 
 struct Workspace {
-    int64_t p, c, n, terms, bytes;
+    int64_t p, c, n, terms, n_terms, bytes;
 };
 Workspace workspace_of(const ficco_expert_balance_t &o)
 {
@@ -295,7 +359,8 @@ Workspace workspace_of(const ficco_expert_balance_t &o)
         w.c = take(c.groups * c.per_group * o.experts * 4);
         w.n = take(c.groups * c.per_group * 4);
     }
-    if (c.groups > 1) w.terms = take(c.groups * 4);
+    w.n_terms = c.groups * (c.per_group > 1 ? (o.experts + 63) / 64 : 1);
+    if (w.n_terms > 1) w.terms = take(w.n_terms * 4);
     w.bytes = at;
     return w;
 }
@@ -315,26 +380,28 @@ BalanceLaunch launch_of(const ficco_expert_balance_t &o, const Chunks &c)
     return a;
 }
 
-template <class L, int LANES, int V>
+template <class L, int LANES, int V, bool FOURS>
 int launch_t(const BalanceLaunch &a, bool backward, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.groups * a.per_group)), block(256);
-    if (backward) hipLaunchKernelGGL((balance_backward_kernel<L, LANES, V>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((balance_kernel<L, LANES, V>), grid, block, (256 * V + a.experts) * 4, s, a);
+    if (backward) hipLaunchKernelGGL((balance_backward_kernel<L, LANES, V, FOURS>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((balance_kernel<L, LANES, V, FOURS>), grid, block, (256 * V + a.experts) * 4, s, a);
     HIP_TRY(hipGetLastError());
     return FICCO_OK;
 }
 template <class L>
 int launch(const BalanceLaunch &a, bool backward, hipStream_t s)
 {
-    if (a.experts <= 8) return launch_t<L, 8, 1>(a, backward, s);
-    if (a.experts <= 16) return launch_t<L, 16, 1>(a, backward, s);
-    if (a.experts <= 32) return launch_t<L, 32, 1>(a, backward, s);
-    if (a.experts <= 64) return launch_t<L, 64, 1>(a, backward, s);
-    if (a.experts <= 128) return launch_t<L, 64, 2>(a, backward, s);
-    if (a.experts <= 256) return launch_t<L, 64, 4>(a, backward, s);
-    if (a.experts <= 512) return launch_t<L, 64, 8>(a, backward, s);
-    return launch_t<L, 64, 16>(a, backward, s);
+    // whole fours of logits where a lane has four or more and every row lies so
+    const bool fours = a.experts % 4 == 0 && a.ld % 4 == 0 && (uintptr_t)a.logits % (4 * sizeof(L)) == 0 && (uintptr_t)a.dlogits % (4 * sizeof(L)) == 0;
+    if (a.experts <= 8) return launch_t<L, 8, 1, false>(a, backward, s);
+    if (a.experts <= 16) return launch_t<L, 16, 1, false>(a, backward, s);
+    if (a.experts <= 32) return launch_t<L, 32, 1, false>(a, backward, s);
+    if (a.experts <= 64) return launch_t<L, 64, 1, false>(a, backward, s);
+    if (a.experts <= 128) return launch_t<L, 64, 2, false>(a, backward, s);
+    if (a.experts <= 256) return fours ? launch_t<L, 64, 4, true>(a, backward, s) : launch_t<L, 64, 4, false>(a, backward, s);
+    if (a.experts <= 512) return fours ? launch_t<L, 64, 8, true>(a, backward, s) : launch_t<L, 64, 8, false>(a, backward, s);
+    return fours ? launch_t<L, 64, 16, true>(a, backward, s) : launch_t<L, 64, 16, false>(a, backward, s);
 }
 
 int forward(const ficco_expert_balance_t *op, const void *logits, const void *ids, const void *valid, void *counts, void *group_valid, void *loss,
@@ -368,16 +435,15 @@ int forward(const ficco_expert_balance_t *op, const void *logits, const void *id
     a.part_c = (int32_t *)(ws + w.c);
     a.part_n = (int32_t *)(ws + w.n);
     a.terms = (float *)(ws + w.terms);
+    a.n_terms = (int32_t)w.n_terms;
     rc = o.logits_type == FICCO_F32 ? launch<float>(a, false, s) : launch<uint16_t>(a, false, s);
     if (rc) return rc;
     if (c.per_group > 1) {
-        int columns = 8;
-        while (columns < o.experts) columns *= 2;
-        hipLaunchKernelGGL(balance_group_kernel, dim3((unsigned)c.groups), dim3(1024), 0, s, a, columns);
+        hipLaunchKernelGGL(balance_group_kernel, dim3((unsigned)c.groups, (unsigned)((o.experts + 63) / 64)), dim3(1024), 0, s, a);
         HIP_TRY(hipGetLastError());
     }
-    if (loss && c.groups > 1) {
-        hipLaunchKernelGGL(balance_loss_kernel, dim3(1), dim3(1024), 0, s, a.terms, (int)c.groups, (float *)loss);
+    if (loss && w.n_terms > 1) {
+        hipLaunchKernelGGL(balance_loss_kernel, dim3(1), dim3(1024), 0, s, a.terms, a.n_terms, (float *)loss);
         HIP_TRY(hipGetLastError());
     }
     return FICCO_OK;

@@ -104,6 +104,145 @@ int tile_for(int64_t M, int64_t K, int64_t N, double *us)
     return choose_tile(&shape, compute_units(), false, us);
 }
 
+// ------------------------------------------------------------------------------------------------------------ few rows
+// A product of a few rows is the weight's way through the chip, once, and where that is short, the latency of one load and of
+// one join. A workgroup has a tile of 16 FM rows x 16 NB columns and all of k, its 8 wavefronts an eighth of k each: fragments come
+// straight from memory into registers (both operands have k contiguous, nothing is shared between wavefronts), U k-tiles
+// at a time, the next U on their way while these are multiplied; the eight partial tiles are added through LDS, in the order
+// of k. So narrow tiles over all of k, instead of wide ones, spread the weight over as many CUs as there are.
+template <int FM_, int NB_>
+struct RowsCfg {
+    static constexpr int FM = FM_, NB = NB_, WAVES = 8, U = FM + NB <= 2 ? 4 : FM + NB <= 3 ? 2 : 1;
+};
+constexpr int kRowsThreads = 512;
+
+template <class T>
+__global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch a)
+{
+    __shared__ f32x4_t s_part[T::WAVES][T::FM * T::NB][64];
+    const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), j = lane & 15, g = lane >> 4;
+    // tiles in 8 runs, one per XCD, rows fastest: the row tiles that read the same columns of the weight share an L2
+    const int tiles_m = (a.M + 16 * T::FM - 1) / (16 * T::FM), tiles_n = (a.N + 16 * T::NB - 1) / (16 * T::NB);
+    const XcdRun run = xcd_run(blockIdx.x, gridDim.x, tiles_m * tiles_n);
+    const int lid = run.start + run.first;
+    const int row0 = lid % tiles_m * 16 * T::FM, col0 = lid / tiles_m * 16 * T::NB;
+    const int pairs = a.K / kBK, first = wave * pairs / T::WAVES, last = (wave + 1) * pairs / T::WAVES;
+    const uint16_t *pa[T::FM], *pw[T::NB];                     // rows and columns that are not there: the last that is
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) pa[i] = a.A + (int64_t)min(row0 + 16 * i + j, a.M - 1) * a.lda + g * 8;
+#pragma unroll
+    for (int n = 0; n < T::NB; ++n) pw[n] = a.Wt + (int64_t)min(col0 + 16 * n + j, a.N - 1) * a.K + g * 8;
+    f32x4_t acc[T::FM][T::NB];
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+        for (int n = 0; n < T::NB; ++n) acc[i][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    struct Frags {
+        bf16x8_t a[T::U][2][T::FM], w[T::U][2][T::NB];
+    } f0, f1;
+    auto load = [&](Frags &f, int p0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < T::U; ++u) {
+            const int64_t k = (int64_t)min(p0 + u, last - 1) * kBK;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int n = 0; n < T::NB; ++n) f.w[u][h][n] = *reinterpret_cast<const bf16x8_t *>(pw[n] + k + 32 * h);
+#pragma unroll
+                for (int i = 0; i < T::FM; ++i) f.a[u][h][i] = *reinterpret_cast<const bf16x8_t *>(pa[i] + k + 32 * h);
+            }
+        }
+    };
+    auto multiply = [&](const Frags &f, int p0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < T::U; ++u)
+            if (p0 + u < last) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+                        for (int n = 0; n < T::NB; ++n)
+                            acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.w[u][h][n], f.a[u][h][i], acc[i][n], 0, 0, 0);
+            }
+    };
+    if (first < last) {
+        load(f0, first);
+        for (int p = first;;) {
+            if (p + T::U < last) load(f1, p + T::U);
+            multiply(f0, p);
+            if ((p += T::U) >= last) break;
+            if (p + T::U < last) load(f0, p + T::U);
+            multiply(f1, p);
+            if ((p += T::U) >= last) break;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+        for (int n = 0; n < T::NB; ++n) s_part[wave][i * T::NB + n][lane] = acc[i][n];
+    __syncthreads();
+    for (int q = wave; q < T::FM * T::NB; q += T::WAVES) {
+        f32x4_t z = s_part[0][q][lane];
+#pragma unroll
+        for (int w = 1; w < T::WAVES; ++w) {
+            const f32x4_t t = s_part[w][q][lane];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) z[v] += t[v];
+        }
+        // z[v] is C[row0 + 16 i + lane % 16][col0 + 16 n + 4 (lane / 16) + v]; N is a multiple of 8
+        const int64_t m = row0 + 16 * (q / T::NB) + j;
+        const int n = col0 + 16 * (q % T::NB) + 4 * g;
+        if (m < a.M && n < a.N) {
+            const f32x4_t bias = bias4(a.e, n);
+            with_activation(a.e.activation, [&](auto act) __attribute__((always_inline)) { store4<act.value>(a.e, z, bias, a.C + m * a.ldc + n, m, n); });
+        }
+    }
+}
+
+template <class T>
+int launch_rows_t(const LinearLaunch &a, hipStream_t s)
+{
+    const int64_t tiles = ((a.M + 16 * T::FM - 1) / (16 * T::FM)) * (((int64_t)a.N + 16 * T::NB - 1) / (16 * T::NB));
+    if (tiles > 0x7FFFFFFF / kRowsThreads) return FICCO_ERR_SHAPE;
+    hipLaunchKernelGGL(linear_rows_kernel<T>, dim3((unsigned)tiles), dim3(kRowsThreads), 0, s, a);
+    HIP_TRY(hipGetLastError());
+    return FICCO_OK;
+}
+
+// Tiles of the few-rows kernel: 16 fm rows x 16 nb columns
+#define FICCO_FOR_EACH_ROWS(X) X(1, 1) X(1, 2) X(1, 4) X(2, 1) X(2, 2) X(4, 1)
+int launch_rows(int fm, int nb, const LinearLaunch &a, hipStream_t s)
+{
+#define X(FM, NB) if (fm == FM && nb == NB) return launch_rows_t<RowsCfg<FM, NB>>(a, s);
+    FICCO_FOR_EACH_ROWS(X)
+#undef X
+    return FICCO_ERR_ARG;
+}
+
+// The few-rows kernel's tile, if it is expected to be faster than the other kernels' estimate (us); fm = 0: it is not. A round of
+// its tiles takes what a CU draws, about 110 KB a us, of its rows and columns over all of k; a launch cannot be faster than the
+// weight's way from memory.
+struct RowsTile {
+    int fm, nb;
+};
+RowsTile rows_tile(int64_t M, int64_t K, int64_t N, double us)
+{
+    RowsTile best{0, 0};
+    if (M > 256) return best;
+    const int cus = compute_units();
+#define X(FM, NB)                                                                                                                        \
+    {                                                                                                                                    \
+        const int64_t tm = (M + 16 * FM - 1) / (16 * FM), tn = (N + 16 * NB - 1) / (16 * NB), rounds = (tm * tn + cus - 1) / cus;        \
+        const double drawn = (double)rounds * (16 * NB + (double)std::min<int64_t>(M, 16 * FM)) * (double)K * 2.0 / 110e3;               \
+        const double t = 2.5 + std::max(drawn, (double)(N * K + M * K) * 2.0 / 4.9e6);                                                   \
+        if ((FM == 1 || M > 16 * FM / 2) && t < us) { us = t; best = {FM, NB}; }                                                         \
+    }
+    FICCO_FOR_EACH_ROWS(X)
+#undef X
+    return best;
+}
+
 // ---------------------------------------------------------------------------------------------- turned operands, dZ
 // src [R][Cc] (stride ld), 64 x 64 values a wavefront: a lane holds 8 rows x 8 columns, loads 16 bytes of each of 8 rows, turns
 // the block with byte permutes and stores 16 bytes of each of 8 columns, so that loads and stores are whole 128-byte lines.
@@ -120,51 +259,82 @@ struct TurnLaunch {
 };
 constexpr int kTurnRows = 256;
 
+// 16 bytes at `off` bytes from a uniform address, which stays in scalar registers
+static __device__ __forceinline__ u32x4_t load_at(const uint16_t *base, uint32_t off)
+{
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(reinterpret_cast<const char *>(base) + off));
+}
+static __device__ __forceinline__ void store_at(uint16_t *base, uint32_t off, u32x4_t v)
+{
+    *reinterpret_cast<u32x4_t *>(reinterpret_cast<char *>(base) + off) = v;
+}
+
 template <int ACT>
 __global__ __launch_bounds__(256) void turn_kernel(TurnLaunch a)
 {
     __shared__ float s_sum[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t r0 = (int64_t)blockIdx.y * kTurnRows + wave * 64 + (lane & 7) * 8;
-    const int64_t c0 = (int64_t)blockIdx.x * 64 + (lane >> 3) * 8;
+    const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6);
+    // the wavefront's place, and the lane's in it
+    const int64_t R0 = (int64_t)blockIdx.y * kTurnRows + wave * 64, C0 = (int64_t)blockIdx.x * 64;
+    const int lr = (lane & 7) * 8, lc = (lane >> 3) * 8;
+    const int rows = (int)min((int64_t)64, a.R - R0), cols = (int)min((int64_t)64, a.Cc - C0);     // of the wavefront's, that exist
+    const bool in = lc < cols;
     u32x4_t v[8];
     float sum[8];
 #pragma unroll
     for (int c = 0; c < 8; ++c) sum[c] = 0.f;
+    if (rows <= 0) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        v[i] = u32x4_t{0u, 0u, 0u, 0u};
-        if (r0 + i < a.R && c0 < a.Cc) v[i] = *reinterpret_cast<const u32x4_t *>(a.src + (r0 + i) * a.ld + c0);
-    }
-    if constexpr (ACT != FICCO_ACT_NONE) {
-        u32x4_t zz[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            zz[i] = u32x4_t{0u, 0u, 0u, 0u};
-            if (r0 + i < a.R && c0 < a.Cc) zz[i] = *reinterpret_cast<const u32x4_t *>(a.z + (r0 + i) * a.ldz + c0);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {
-                const float lo = bf16_lo(v[i][p]) * slope<ACT>(bf16_lo(zz[i][p])), hi = bf16_hi(v[i][p]) * slope<ACT>(bf16_hi(zz[i][p]));
-                const bool there = r0 + i < a.R && c0 < a.Cc;
-                sum[2 * p] += there ? lo : 0.f;
-                sum[2 * p + 1] += there ? hi : 0.f;
-                v[i][p] = there ? pack2_bf16_rne(lo, hi) : 0u;
-            }
+        for (int i = 0; i < 8; ++i) v[i] = u32x4_t{0u, 0u, 0u, 0u};
     } else {
+        // rows and columns that are not there are read at the last that is, and then put to zero: a load under a condition of
+        // its own makes the compiler copy all the others
+        const uint16_t *src = a.src + R0 * a.ld + C0;
+        const uint32_t c2 = (uint32_t)min(lc, cols - 8) * 2u;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = load_at(src, (uint32_t)min(lr + i, rows - 1) * ((uint32_t)a.ld * 2u) + c2);
+        u32x4_t zz[8];
+        if constexpr (ACT != FICCO_ACT_NONE) {
+            const uint16_t *z = a.z + R0 * a.ldz + C0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) zz[i] = load_at(z, (uint32_t)min(lr + i, rows - 1) * ((uint32_t)a.ldz * 2u) + c2);
+        }
+        if (rows < 64 || cols < 64) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    v[i][p] = in && lr + i < rows ? v[i][p] : 0u;
+                    if constexpr (ACT != FICCO_ACT_NONE) zz[i][p] = in && lr + i < rows ? zz[i][p] : 0u;
+                }
+        }
+        if constexpr (ACT != FICCO_ACT_NONE) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    const float lo = bf16_lo(v[i][p]) * slope<ACT>(bf16_lo(zz[i][p])), hi = bf16_hi(v[i][p]) * slope<ACT>(bf16_hi(zz[i][p]));
+                    sum[2 * p] += lo;
+                    sum[2 * p + 1] += hi;
+                    v[i][p] = pack2_bf16_rne(lo, hi);
+                }
+        } else if (a.sums) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int p = 0; p < 4; ++p) { sum[2 * p] += bf16_lo(v[i][p]); sum[2 * p + 1] += bf16_hi(v[i][p]); }
+        }
+    }
+    if (a.same && C0 + lc < a.lds) {
+        uint16_t *same = a.same + R0 * a.lds + C0;
+        const uint32_t off = ((uint32_t)lr * (uint32_t)a.lds + (uint32_t)lc) * 2u;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int p = 0; p < 4; ++p) { sum[2 * p] += bf16_lo(v[i][p]); sum[2 * p + 1] += bf16_hi(v[i][p]); }
+            if (lr + i < rows) store_at(same + i * a.lds, off, v[i]);
     }
-    if (a.same) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (r0 + i < a.R && c0 < a.lds) *reinterpret_cast<u32x4_t *>(a.same + (r0 + i) * a.lds + c0) = v[i];
-    }
-    if (a.turned && r0 < a.ldt && c0 < a.Cc) {
+    if (a.turned && R0 + lr < a.ldt && in) {
+        uint16_t *turned = a.turned + C0 * a.ldt + R0;
+        const uint32_t off = ((uint32_t)lc * (uint32_t)a.ldt + (uint32_t)lr) * 2u;
 #pragma unroll
         for (int p = 0; p < 4; ++p) {
             u32x4_t even, odd;
@@ -173,8 +343,8 @@ __global__ __launch_bounds__(256) void turn_kernel(TurnLaunch a)
                 even[i] = __builtin_amdgcn_perm(v[2 * i + 1][p], v[2 * i][p], 0x05040100u);
                 odd[i] = __builtin_amdgcn_perm(v[2 * i + 1][p], v[2 * i][p], 0x07060302u);
             }
-            *reinterpret_cast<u32x4_t *>(a.turned + (c0 + 2 * p) * a.ldt + r0) = even;
-            *reinterpret_cast<u32x4_t *>(a.turned + (c0 + 2 * p + 1) * a.ldt + r0) = odd;
+            store_at(turned + 2 * p * a.ldt, off, even);
+            store_at(turned + (2 * p + 1) * a.ldt, off, odd);
         }
     }
     if (a.sums) {
@@ -184,9 +354,9 @@ __global__ __launch_bounds__(256) void turn_kernel(TurnLaunch a)
             for (int m = 1; m < 8; m <<= 1) sum[c] += __shfl_xor(sum[c], m, 64);
         if ((lane & 7) == 0)
 #pragma unroll
-            for (int c = 0; c < 8; ++c) s_sum[wave][(lane >> 3) * 8 + c] = sum[c];
+            for (int c = 0; c < 8; ++c) s_sum[wave][lc + c] = sum[c];
         __syncthreads();
-        const int64_t c = (int64_t)blockIdx.x * 64 + threadIdx.x;
+        const int64_t c = C0 + threadIdx.x;
         if (threadIdx.x < 64 && c < a.Cc)
             a.sums[(int64_t)blockIdx.y * a.Cc + c] = (s_sum[0][threadIdx.x] + s_sum[1][threadIdx.x]) + (s_sum[2][threadIdx.x] + s_sum[3][threadIdx.x]);
     }
@@ -246,27 +416,31 @@ int checked(const ficco_linear_t *op, bool backward, ficco_linear_t *out)
     if (!o.ldc) o.ldc = o.N;
     if (!o.ld_residual) o.ld_residual = o.N;
     if (!o.ld_pre) o.ld_pre = o.N;
-    if (o.lda < o.K || o.lda % 8 || o.lda > kMaxK || o.ldc < o.N || o.ldc % 8 || o.ldc > kMaxK || o.ld_residual < o.N || o.ld_residual % 8 || o.ld_pre < o.N ||
-        o.ld_pre % 8)
+    if (o.lda < o.K || o.lda % 8 || o.lda > kMaxK || o.ldc < o.N || o.ldc % 8 || o.ldc > kMaxK || o.ld_residual < o.N || o.ld_residual % 8 || o.ld_residual > kMaxK ||
+        o.ld_pre < o.N || o.ld_pre % 8 || o.ld_pre > kMaxK)
         return FICCO_ERR_SHAPE;
     *out = o;
     return FICCO_OK;
 }
 
-// How a forward goes: row blocks of the direct kernel, which takes the [K,N] weight as it is, or 0 and the tile of the others.
+// How a forward goes: row blocks of the direct kernel, which takes a [K,N] weight as it is; or the few-rows kernel's tile for an [N,K]
+// one; or the others' tile.
 struct Forward {
     int row_blocks, tile;
+    RowsTile rows;
     int64_t bytes;
 };
 Forward forward_way(const ficco_linear_t &o)
 {
-    Forward f{0, 0, 0};
+    Forward f{};
     if (o.M == 0) return f;
     double us = 0;
     f.tile = tile_for(o.M, o.K, o.N, &us);
     if (o.weight_layout == FICCO_WEIGHT_KN) {
         if (o.K * o.N * 2 <= 0x7FFFFFFF) f.row_blocks = direct_row_blocks(o.M, o.K, o.N, compute_units(), us);
         if (!f.row_blocks) f.bytes = round_up(o.K * o.N * 2, 256);
+    } else {
+        f.rows = rows_tile(o.M, o.K, o.N, us);
     }
     return f;
 }
@@ -355,7 +529,7 @@ int forward(const ficco_linear_t *op, const void *A, const void *W, const void *
         wt = (const uint16_t *)workspace;
     }
     const LinearLaunch a{(const uint16_t *)A, wt, (uint16_t *)C, o.lda, o.ldc, (int32_t)o.M, (int32_t)o.N, (int32_t)o.K, 0, e};
-    return launch_tiles(f.tile, a, s);
+    return f.rows.fm ? launch_rows(f.rows.fm, f.rows.nb, a, s) : launch_tiles(f.tile, a, s);
 }
 
 int backward(const ficco_linear_t *op, const void *A, const void *W, const void *pre, const void *dC, void *dA, void *dW, void *dbias, void *workspace,

@@ -8,6 +8,7 @@
 // between its loads and its stores, and is read once. All sums are fp32.
 #include "ficco_operators.h"
 #include "ficco_epilogue.h"
+#include "ficco_lanes.h"
 
 namespace ficco {
 namespace {
@@ -70,45 +71,26 @@ static __device__ __forceinline__ void store8(void *p, int64_t at, const Vec8 &v
     }
 }
 
-// Sums of N values over the TPR threads of a row; every thread gets them. `s`: N floats for each of the row's wavefronts, not
-// in use by an earlier call that a wavefront may still read.
-template <int TPR, int N>
-static __device__ __forceinline__ void row_sum(float (&v)[N], float *s)
-{
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1)
-#pragma unroll
-        for (int k = 0; k < N; ++k) v[k] += __shfl_xor(v[k], m, 64);
-    if constexpr (TPR > 64) {
-        if ((threadIdx.x & 63) == 0)
-#pragma unroll
-            for (int k = 0; k < N; ++k) s[(threadIdx.x >> 6) * N + k] = v[k];
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            float t = 0.f;
-#pragma unroll
-            for (int w = 0; w < TPR / 64; ++w) t += s[w * N + k];
-            v[k] = t;
-        }
-    }
-}
-
 // TPR threads a row (a wavefront, with four rows a workgroup, or a whole workgroup), V vectors of 8 values a thread.
 template <int TPR, int V>
 struct RowCfg {
-    static constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
+    static constexpr int THREADS = TPR == 64 ? 256 : TPR, ROWS = THREADS / TPR;
+    static_assert(ROWS == 1 || TPR == 64, "a row's number is the same in a whole wavefront");
+    static __device__ __forceinline__ int lane() { return ROWS == 1 ? threadIdx.x : threadIdx.x % 64; }
+    static __device__ __forceinline__ int row() { return ROWS == 1 ? 0 : scalar(threadIdx.x / 64); }
 };
 
 template <int TPR, int V, bool F32>
 __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS)) void residual_norm_kernel(NormLaunch a)
 {
-    constexpr int ROWS = RowCfg<TPR, V>::ROWS;
-    __shared__ float s_post[TPR / 64], s_pre[TPR / 64];
-    const int lane = threadIdx.x % TPR;
+    typedef RowCfg<TPR, V> R;
+    constexpr int ROWS = R::ROWS;
+    __shared__ float s_post[2][16], s_pre[2][16];
+    const int lane = R::lane();
     const float inv = 1.0f / (float)a.width;
     const int vecs = a.width / 8;
-    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * ROWS) {
+    int turn = 0;                          // the sums' places in turns, so that they are not those a slower wavefront still reads
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + R::row(); row < a.rows; row += (int64_t)gridDim.x * ROWS, turn ^= 1) {
         const int64_t at = row * a.width;
         const int64_t gate_at = a.gate && a.gate_rows ? (int64_t)((int)row / a.gate_rows) * a.width : 0;
         u32x4_t b[V];
@@ -134,7 +116,7 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS)) void residual_norm_kerne
 #pragma unroll
                 for (int e = 0; e < 8; ++e) ss[0] = fmaf(w.f[e], w.f[e], ss[0]);
             }
-            row_sum<TPR, 1>(ss, s_post);
+            thread_sums<TPR, 1>(ss, s_post[turn]);
             r = rsqrtf(fmaf(ss[0], inv, a.eps));
         }
         float ss[1] = {0.f};
@@ -162,7 +144,7 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS)) void residual_norm_kerne
             }
         }
         if (a.h) {
-            row_sum<TPR, 1>(ss, s_pre);
+            thread_sums<TPR, 1>(ss, s_pre[turn]);
             r = rsqrtf(fmaf(ss[0], inv, a.eps));
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -175,18 +157,46 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS)) void residual_norm_kerne
                 }
             }
         }
-        if constexpr (TPR > 64) __syncthreads();       // the sums' places are used again
     }
 }
 
-// The backward's rows go in chunks, each walked by one group of TPR threads, which keeps its columns' partial sums in registers
-// and writes them once: sums over rows in a fixed order, without atomics.
-template <int TPR, int V, bool F32>
-__global__ __launch_bounds__((RowCfg<TPR, V>::THREADS)) void residual_norm_backward_kernel(NormLaunch a)
+// What a thread loads of a row for one vector, as it comes
+template <bool F32>
+struct RawRow {
+    u32x4_t y[F32 ? 2 : 1], dy[F32 ? 2 : 1], b, dh;
+};
+template <bool F32>
+static __device__ __forceinline__ void load_raw(u32x4_t (&r)[F32 ? 2 : 1], const void *p, int64_t at)
 {
-    constexpr int ROWS = RowCfg<TPR, V>::ROWS;
-    __shared__ float s_a[3 * (TPR / 64)], s_b[TPR / 64];
-    const int lane = threadIdx.x % TPR, chunk = blockIdx.x * ROWS + threadIdx.x / TPR;
+    const u32x4_t *v = reinterpret_cast<const u32x4_t *>(static_cast<const char *>(p) + at * (F32 ? 4 : 2));
+    r[0] = __builtin_nontemporal_load(v);
+    if constexpr (F32) r[1] = __builtin_nontemporal_load(v + 1);
+}
+template <bool F32>
+static __device__ __forceinline__ Vec8 widen_raw(const u32x4_t (&r)[F32 ? 2 : 1])
+{
+    if constexpr (F32) {
+        Vec8 o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { o.f[i] = __uint_as_float(r[0][i]); o.f[4 + i] = __uint_as_float(r[1][i]); }
+        return o;
+    } else return widen(r[0]);
+}
+
+// The backward's rows go in chunks, each walked by one group of TPR threads, which keeps its columns' partial sums in registers
+// and writes them once: sums over rows in a fixed order, without atomics. A row needs two sums over its columns in turn, the
+// second of what the first gives, so the next row is loaded before the first: its way from memory is then behind both. What a
+// thread past the row's end loads is the row's first vector, and nothing comes of it.
+template <int TPR, int V, bool F32>
+__global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), 4) void residual_norm_backward_kernel(NormLaunch a)
+{
+    typedef RowCfg<TPR, V> R;
+    constexpr int ROWS = R::ROWS;
+    // One vector a thread: the parameters stay in 128 registers, and the next row is loaded early. Two: neither has room, and a row is
+    // loaded again where it is used again.
+    constexpr bool KEEP = V == 1;
+    __shared__ float s_a[2][3 * 16], s_b[2][16];      // in turns, so that a row's places are not those a slower wavefront still reads
+    const int lane = R::lane(), chunk = blockIdx.x * ROWS + R::row();
     if (TPR == 64 && chunk >= a.chunks) return;
     const float inv = 1.0f / (float)a.width;
     const int vecs = a.width / 8;
@@ -197,114 +207,141 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS)) void residual_norm_backw
         end = min(begin + a.chunk_rows, (int64_t)(g + 1) * a.gate_rows);
     }
     end = min(end, (int64_t)a.rows);
-    Vec8 dpost[V], dgate[V], dpre[V];
+    int col[V];
+    float there[V];                        // 1, or 0 past the row's end
 #pragma unroll
-    for (int v = 0; v < V; ++v) dpost[v] = dgate[v] = dpre[v] = Vec8{};
+    for (int v = 0; v < V; ++v) {
+        const bool in = lane + v * TPR < vecs;
+        col[v] = in ? (lane + v * TPR) * 8 : 0;
+        there[v] = in ? 1.0f : 0.0f;
+    }
+    const bool has_dh = a.dh != nullptr, has_dy = a.dy != nullptr, has_b = a.block != nullptr, post = a.post != nullptr, gated = a.gate != nullptr;
+    Vec8 dpost[V], dgate[V], dpre[V], w[V], p[V], gt[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) dpost[v] = dgate[v] = dpre[v] = w[v] = p[v] = gt[v] = Vec8{};
+    auto params = [&](int v) __attribute__((always_inline)) {
+        if (has_dh) w[v] = param8(a.pre, a.param_f32, col[v]);
+        if (post) p[v] = param8(a.post, a.param_f32, col[v]);
+    };
+    if constexpr (KEEP) params(0);
+    auto load = [&](RawRow<F32> &raw, int64_t row, int v) __attribute__((always_inline)) {
+        const int64_t at = row * a.width + col[v];
+        if (has_dh) {
+            load_raw<F32>(raw.y, a.x, at);
+            raw.dh = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(a.dh + at));
+        }
+        if (has_dy) load_raw<F32>(raw.dy, a.dy, at);
+        if (has_b) raw.b = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(a.block + at));
+    };
+    RawRow<F32> next{};
+    if (KEEP && begin < end) load(next, begin, 0);
+    int group = a.gate_rows ? (int)(begin / a.gate_rows) : 0, group_end = a.gate_rows ? (int)min((int64_t)(group + 1) * a.gate_rows, (int64_t)a.rows) : a.rows;
+    bool new_gate = true;
     for (int64_t row = begin; row < end; ++row) {
         const int64_t at = row * a.width;
-        const int group = a.gate_rows ? (int)row / a.gate_rows : 0;
-        const int64_t gate_at = (int64_t)group * a.width;
-        Vec8 d[V], y[V], b[V], dh[V];      // d: dy, then dY, then post * dn
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int i = lane + v * TPR;
-            d[v] = y[v] = b[v] = dh[v] = Vec8{};
-            if (i < vecs) {
-                if (a.dy) d[v] = load8<F32>(a.dy, at + i * 8);
-                if (a.dh) { y[v] = load8<F32>(a.x, at + i * 8); dh[v] = load8<false>(a.dh, at + i * 8); }
-                if (a.block) b[v] = load8<false>(a.block, at + i * 8);
-            }
-        }
+        const int parity = (int)(row - begin) & 1;
+        RawRow<F32> now = next;
+        Vec8 d[V];                         // dy, then dY, then post * dn
         float s[3] = {0.f, 0.f, 0.f};      // y^2, u y, b^2
+        if (KEEP && gated && new_gate) gt[0] = param8(a.gate, a.param_f32, (int64_t)group * a.width + col[0]);
+        new_gate = false;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int i = lane + v * TPR;
-            if (i < vecs) {
-                if (a.dh) {
-                    const Vec8 w = param8(a.pre, a.param_f32, i * 8);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        s[0] = fmaf(y[v].f[e], y[v].f[e], s[0]);
-                        s[1] = fmaf(w.f[e] * dh[v].f[e], y[v].f[e], s[1]);
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s[2] = fmaf(b[v].f[e], b[v].f[e], s[2]);
+            if constexpr (!KEEP) {
+                params(v);
+                load(now, row, v);
             }
+            const Vec8 y = widen_raw<F32>(now.y), b = widen(now.b), dh = widen(now.dh);
+            float t[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                t[0] = fmaf(y.f[e], y.f[e], t[0]);
+                t[1] = fmaf(w[v].f[e] * dh.f[e], y.f[e], t[1]);
+                t[2] = fmaf(b.f[e], b.f[e], t[2]);
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) s[k] += there[v] != 0.f ? t[k] : 0.f;
         }
-        row_sum<TPR, 3>(s, s_a);
+        if (KEEP && row + 1 < end) load(next, row + 1, 0);
+        thread_sums<TPR, 3>(s, s_a[parity]);
         const float r = rsqrtf(fmaf(s[0], inv, a.eps)), back = r * r * r * s[1] * inv;
-        const float rb = a.post ? rsqrtf(fmaf(s[2], inv, a.eps)) : 1.0f;
+        const float rb = post ? rsqrtf(fmaf(s[2], inv, a.eps)) : 1.0f;
         float s4[1] = {0.f};
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int i = lane + v * TPR;
-            if (i < vecs) {
-                if (a.dh) {
-                    const Vec8 w = param8(a.pre, a.param_f32, i * 8);
+            const bool in = there[v] != 0.f;
+            if constexpr (!KEEP) {
+                params(v);
+                if (gated) gt[v] = param8(a.gate, a.param_f32, (int64_t)group * a.width + col[v]);
+                load(now, row, v);
+            }
+            d[v] = widen_raw<F32>(now.dy);
+            const Vec8 b = widen(now.b);
+            if (has_dh) {
+                const Vec8 y = widen_raw<F32>(now.y), dh = widen(now.dh);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        d[v].f[e] += fmaf(r * w.f[e], dh[v].f[e], -y[v].f[e] * back);
-                        dpre[v].f[e] = fmaf(dh[v].f[e] * r, y[v].f[e], dpre[v].f[e]);
-                    }
-                }
-                if (a.y) {
-                    Vec8 o;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) o.f[e] = a.scale * d[v].f[e];
-                    store8<F32>(a.y, at + i * 8, o);
-                }
-                Vec8 p = Vec8{};
-                if (a.post) p = param8(a.post, a.param_f32, i * 8);
-                if (a.gate) {
-                    const Vec8 g = param8(a.gate, a.param_f32, gate_at + i * 8);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float n = a.post ? b[v].f[e] * rb * p.f[e] : b[v].f[e];
-                        dgate[v].f[e] = fmaf(d[v].f[e], n, dgate[v].f[e]);
-                        d[v].f[e] *= g.f[e];
-                    }
-                }
-                if (a.post) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        dpost[v].f[e] = fmaf(d[v].f[e], b[v].f[e] * rb, dpost[v].f[e]);
-                        d[v].f[e] *= p.f[e];
-                        s4[0] = fmaf(d[v].f[e], b[v].f[e], s4[0]);
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    d[v].f[e] += fmaf(r * w[v].f[e], dh.f[e], -y.f[e] * back);
+                    dpre[v].f[e] = fmaf(dh.f[e] * r, y.f[e], dpre[v].f[e]);
                 }
             }
+            if (a.y && in) {
+                Vec8 o;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o.f[e] = a.scale * d[v].f[e];
+                store8<F32>(a.y, at + col[v], o);
+            }
+            if (gated) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float n = post ? b.f[e] * rb * p[v].f[e] : b.f[e];
+                    dgate[v].f[e] = fmaf(d[v].f[e], n, dgate[v].f[e]);
+                    d[v].f[e] *= gt[v].f[e];
+                }
+            }
+            if (post) {
+                float t = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    dpost[v].f[e] = fmaf(d[v].f[e], b.f[e] * rb, dpost[v].f[e]);
+                    d[v].f[e] *= p[v].f[e];
+                    t = fmaf(d[v].f[e], b.f[e], t);
+                }
+                s4[0] += in ? t : 0.f;
+            }
         }
-        if (a.post) row_sum<TPR, 1>(s4, s_b);
+        if (post) thread_sums<TPR, 1>(s4, s_b[parity]);
         if (a.h) {
             const float back_b = rb * rb * rb * s4[0] * inv;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int i = lane + v * TPR;
-                if (i < vecs) {
-                    if (a.post)
+                if (post) {
+                    if constexpr (!KEEP) now.b = *reinterpret_cast<const u32x4_t *>(a.block + at + col[v]);
+                    const Vec8 b = widen(now.b);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) d[v].f[e] = fmaf(rb, d[v].f[e], -b[v].f[e] * back_b);
-                    store8<false>(a.h, at + i * 8, d[v]);
+                    for (int e = 0; e < 8; ++e) d[v].f[e] = fmaf(rb, d[v].f[e], -b.f[e] * back_b);
                 }
+                if (there[v] != 0.f) store8<false>(a.h, at + col[v], d[v]);
             }
         }
-        // a group of rows that share a gate ends inside the chunk: it lies in it whole
-        if (a.dgate && (row + 1 == end || (int)(row + 1) / a.gate_rows != group)) {
+        if (row + 1 == group_end && a.gate_rows) {
+            // a group of rows that share a gate ends; where a chunk holds whole groups it writes their sums
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int i = lane + v * TPR;
-                if (i < vecs) store8<true>(a.dgate, gate_at + i * 8, dgate[v]);
-                dgate[v] = Vec8{};
+                if (a.dgate) {
+                    if (there[v] != 0.f) store8<true>(a.dgate, (int64_t)group * a.width + col[v], dgate[v]);
+                    dgate[v] = Vec8{};
+                }
             }
+            ++group;
+            group_end = (int)min((int64_t)group_end + a.gate_rows, (int64_t)a.rows);
+            new_gate = true;
         }
-        if constexpr (TPR > 64) __syncthreads();       // the sums' places are used again
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int i = lane + v * TPR;
-        if (i < vecs) {
-            const int64_t plane = (int64_t)a.chunks * a.width, at = (int64_t)chunk * a.width + i * 8;
+        if (there[v] != 0.f) {
+            const int64_t plane = (int64_t)a.chunks * a.width, at = (int64_t)chunk * a.width + col[v];
             if (a.want_post) store8<true>(a.sums, at, dpost[v]);
             if (a.want_gate && !a.dgate) store8<true>(a.sums, plane + at, dgate[v]);
             if (a.want_pre) store8<true>(a.sums, 2 * plane + at, dpre[v]);
@@ -355,8 +392,13 @@ int checked(const ficco_residual_norm_t *op, ficco_residual_norm_t *out)
     return FICCO_OK;
 }
 
-// Threads a row in the backward: what its three partial sums and four operands leave room for, V = 1 or 2 vectors a thread.
-int backward_tpr(int64_t width) { return width <= 1024 ? 64 : width <= 4096 ? 256 : width <= 8192 ? 512 : 1024; }
+// Threads a row in the backward: one vector a thread, as far as a workgroup's 1024 threads go.
+int backward_tpr(int64_t width)
+{
+    for (int tpr : {64, 128, 192, 256, 384, 512, 768})
+        if (width <= tpr * 8) return tpr;
+    return 1024;
+}
 
 struct Chunks {
     int64_t chunks, per_group, rows, groups;
@@ -364,9 +406,9 @@ struct Chunks {
 };
 Chunks chunks_of(const ficco_residual_norm_t &o)
 {
-    // two workgroups a CU of 256 CUs
-    const int64_t target = std::max<int64_t>(256, 131072 / backward_tpr(o.width));
-    const int64_t each = std::max<int64_t>(1, (o.rows + target - 1) / target);
+    // as many as run at once on 256 CUs with 1024 threads each; but a chunk's sums are written and read again, so at least four rows
+    const int64_t target = 256 * 1024 / backward_tpr(o.width);
+    const int64_t each = std::max<int64_t>(4, (o.rows + target - 1) / target);
     Chunks c{};
     if (!o.gate_rows || o.gate_rows >= o.rows) {
         c.groups = 1;
@@ -420,17 +462,16 @@ int launch_backward_t(const NormLaunch &a, bool f32, hipStream_t s)
 
 int launch_backward(const NormLaunch &a, bool f32, hipStream_t s)
 {
-    const int tpr = backward_tpr(a.width), v = (a.width / 8 + tpr - 1) / tpr;
-    if (v == 1) {
-        if (tpr == 64) return launch_backward_t<64, 1>(a, f32, s);
-        if (tpr == 256) return launch_backward_t<256, 1>(a, f32, s);
-    } else if (v == 2) {
-        if (tpr == 64) return launch_backward_t<64, 2>(a, f32, s);
-        if (tpr == 256) return launch_backward_t<256, 2>(a, f32, s);
-        if (tpr == 512) return launch_backward_t<512, 2>(a, f32, s);
-        if (tpr == 1024) return launch_backward_t<1024, 2>(a, f32, s);
+    switch (backward_tpr(a.width)) {
+    case 64: return launch_backward_t<64, 1>(a, f32, s);
+    case 128: return launch_backward_t<128, 1>(a, f32, s);
+    case 192: return launch_backward_t<192, 1>(a, f32, s);
+    case 256: return launch_backward_t<256, 1>(a, f32, s);
+    case 384: return launch_backward_t<384, 1>(a, f32, s);
+    case 512: return launch_backward_t<512, 1>(a, f32, s);
+    case 768: return launch_backward_t<768, 1>(a, f32, s);
     }
-    return FICCO_ERR_SHAPE;
+    return a.width <= 8192 ? launch_backward_t<1024, 1>(a, f32, s) : launch_backward_t<1024, 2>(a, f32, s);
 }
 
 int forward(const ficco_residual_norm_t *op, const void *x, const void *block, const void *post, const void *gate, const void *pre, void *y, void *h,

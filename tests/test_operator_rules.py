@@ -23,7 +23,8 @@ def linear(backward=False, **k):
 
 @pytest.mark.parametrize("backward", [False, True])
 @pytest.mark.parametrize("bad", [dict(M=-1), dict(M=1 << 31), dict(K=0), dict(K=96), dict(K=(1 << 22) + 64), dict(N=0), dict(N=12), dict(N=(1 << 22) + 8), dict(lda=56),
-                                 dict(lda=68), dict(lda=(1 << 22) + 8), dict(ldc=56), dict(ldc=68), dict(ld_residual=60), dict(ld_residual=56), dict(ld_pre=60), dict(ld_pre=56)])
+                                 dict(lda=68), dict(lda=(1 << 22) + 8), dict(ldc=56), dict(ldc=68), dict(ld_residual=60), dict(ld_residual=56), dict(ld_pre=60), dict(ld_pre=56),
+                                 dict(ld_pre=(1 << 22) + 8), dict(ld_residual=(1 << 22) + 8)])
 def test_linear_shapes(backward, bad):
     assert linear(backward, **bad) == F.FICCO_ERR_SHAPE
     op = F.ficco_linear_t(**{**dict(M=8, K=64, N=64), **bad})
