@@ -119,8 +119,7 @@ static __device__ __forceinline__ void store4(const Epilogue &e, f32x4_t z, f32x
 
 // tile_store with an epilogue: the exchange between lanes is made with the fp32 values, so that a lane has 8 consecutive
 // columns of a row before bias, activation and residual are applied and everything it reads and writes there is 16 bytes.
-// row0, col0: the tile's place. The residual's values of a row block are loaded one block ahead, since the store before them
-// may be to the same memory and the compiler keeps that order.
+// row0, col0: the tile's place. M 16384, K 8192, N 3584: nothing 709 us, SiLU 717, GELU by tanh 722, by erf 746.
 template <class T, int ACT>
 static __device__ __forceinline__ void tile_store_epilogue(const TileAcc<T> &ta, const Epilogue &e, uint16_t *c_tile, int rows_valid,
                                                            int cols_valid, int64_t ldc, int64_t row0, int col0)
@@ -139,23 +138,22 @@ static __device__ __forceinline__ void tile_store_epilogue(const TileAcc<T> &ta,
         bias[j] = there ? bias4(e, col0 + n) : f32x4_t{0.f, 0.f, 0.f, 0.f};
         bias[j + 1] = there ? bias4(e, col0 + n + 4) : f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
-    u32x4_t res[2][T::FN / 2];
-    auto load_residual = [&](auto i_c) __attribute__((always_inline)) {
-        constexpr int i = decltype(i_c)::value;
-        const int m = wm * T::WTM + i * 16 + frow;
-        const uint16_t *r = e.residual + (row0 + m) * e.ld_residual + col0;
+    // All of the residual's values before the first store (the fragments' registers are free by now): vector memory operations
+    // complete in order, so a load behind a store waits for that store.
+    u32x4_t res[T::FM][T::FN / 2];
+    if (e.residual) {
+        const uint16_t *r0 = e.residual + row0 * e.ld_residual + col0;
 #pragma unroll
-        for (int j = 0; j < T::FN; j += 2)
-            if (m < rows_valid && n0 + j * 16 < cols_valid) res[i % 2][j / 2] = *reinterpret_cast<const u32x4_t *>(r + n0 + j * 16);
-    };
-    if (e.residual) load_residual(std::integral_constant<int, 0>{});
+        for (int i = 0; i < T::FM; ++i) {
+            const uint16_t *r = r0 + (int64_t)min(wm * T::WTM + i * 16 + frow, rows_valid - 1) * e.ld_residual;
+#pragma unroll
+            for (int j = 0; j < T::FN; j += 2) res[i][j / 2] = *reinterpret_cast<const u32x4_t *>(r + min(n0 + j * 16, cols_valid - 8));
+        }
+    }
     static_for<T::FM>([&](auto i_c) __attribute__((always_inline)) {
         constexpr int i = decltype(i_c)::value;
         const int m = wm * T::WTM + i * 16 + frow;
         uint16_t *crow = c_tile + (int64_t)m * ldc;
-        if constexpr (i + 1 < T::FM) {
-            if (e.residual) load_residual(std::integral_constant<int, i + 1>{});
-        }
         static_for<T::FN / 2>([&](auto j_c) __attribute__((always_inline)) {
             constexpr int j = 2 * decltype(j_c)::value;
             float z[8];
@@ -173,7 +171,7 @@ static __device__ __forceinline__ void tile_store_epilogue(const TileAcc<T> &ta,
 #pragma unroll
                 for (int v = 0; v < 8; ++v) z[v] = activate<ACT>(z[v]);
                 if (e.residual) {
-                    const u32x4_t r = res[i % 2][j / 2];
+                    const u32x4_t r = res[i][j / 2];
 #pragma unroll
                     for (int v = 0; v < 4; ++v) { z[2 * v] += bf16_lo(r[v]); z[2 * v + 1] += bf16_hi(r[v]); }
                 }

@@ -106,10 +106,11 @@ int tile_for(int64_t M, int64_t K, int64_t N, double *us)
 
 // ------------------------------------------------------------------------------------------------------------ few rows
 // A product of a few rows is the weight's way through the chip, once, and where that is short, the latency of one load and of
-// one join. A workgroup has a tile of 16 FM rows x 16 NB columns and all of k, its 8 wavefronts an eighth of k each: fragments come
+// one join. A workgroup has a tile of 16 FM rows x 16 NB columns and all of k, its 8 wavefronts every 8th k-tile (128 bytes of a row) each, so that
+// together they read 1 KiB of each row at a time: fragments come
 // straight from memory into registers (both operands have k contiguous, nothing is shared between wavefronts), U k-tiles
 // at a time, the next U on their way while these are multiplied; the eight partial tiles are added through LDS, in the order
-// of k. So narrow tiles over all of k, instead of wide ones, spread the weight over as many CUs as there are.
+// of the wavefronts. So narrow tiles over all of k, instead of wide ones, spread the weight over as many CUs as there are.
 template <int FM_, int NB_>
 struct RowsCfg {
     static constexpr int FM = FM_, NB = NB_, WAVES = 8, U = FM + NB <= 2 ? 4 : FM + NB <= 3 ? 2 : 1;
@@ -126,7 +127,7 @@ __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch 
     const XcdRun run = xcd_run(blockIdx.x, gridDim.x, tiles_m * tiles_n);
     const int lid = run.start + run.first;
     const int row0 = lid % tiles_m * 16 * T::FM, col0 = lid / tiles_m * 16 * T::NB;
-    const int pairs = a.K / kBK, first = wave * pairs / T::WAVES, last = (wave + 1) * pairs / T::WAVES;
+    const int pairs = a.K / kBK;               // k-tiles: the wavefront has every 8th
     const uint16_t *pa[T::FM], *pw[T::NB];                     // rows and columns that are not there: the last that is
 #pragma unroll
     for (int i = 0; i < T::FM; ++i) pa[i] = a.A + (int64_t)min(row0 + 16 * i + j, a.M - 1) * a.lda + g * 8;
@@ -143,7 +144,7 @@ __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch 
     auto load = [&](Frags &f, int p0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < T::U; ++u) {
-            const int64_t k = (int64_t)min(p0 + u, last - 1) * kBK;
+            const int64_t k = (int64_t)min(p0 + u * T::WAVES, pairs - 1) * kBK;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -156,7 +157,7 @@ __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch 
     auto multiply = [&](const Frags &f, int p0) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < T::U; ++u)
-            if (p0 + u < last) {
+            if (p0 + u * T::WAVES < pairs) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -166,15 +167,16 @@ __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch 
                             acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.w[u][h][n], f.a[u][h][i], acc[i][n], 0, 0, 0);
             }
     };
-    if (first < last) {
-        load(f0, first);
-        for (int p = first;;) {
-            if (p + T::U < last) load(f1, p + T::U);
+    constexpr int STEP = T::U * T::WAVES;
+    if (wave < pairs) {
+        load(f0, wave);
+        for (int p = wave;;) {
+            if (p + STEP < pairs) load(f1, p + STEP);
             multiply(f0, p);
-            if ((p += T::U) >= last) break;
-            if (p + T::U < last) load(f0, p + T::U);
+            if ((p += STEP) >= pairs) break;
+            if (p + STEP < pairs) load(f0, p + STEP);
             multiply(f1, p);
-            if ((p += T::U) >= last) break;
+            if ((p += STEP) >= pairs) break;
         }
     }
 #pragma unroll

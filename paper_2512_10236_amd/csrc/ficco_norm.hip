@@ -43,13 +43,16 @@ static __device__ __forceinline__ u32x4_t narrow(const Vec8 &v)
 {
     return u32x4_t{pack2_bf16_rne(v.f[0], v.f[1]), pack2_bf16_rne(v.f[2], v.f[3]), pack2_bf16_rne(v.f[4], v.f[5]), pack2_bf16_rne(v.f[6], v.f[7])};
 }
-static __device__ __forceinline__ Vec8 from_f32(const float *p)
+static __device__ __forceinline__ Vec8 from_f32x4(f32x4_t a, f32x4_t b)
 {
     Vec8 o;
-    const f32x4_t a = reinterpret_cast<const f32x4_t *>(p)[0], b = reinterpret_cast<const f32x4_t *>(p)[1];
 #pragma unroll
     for (int i = 0; i < 4; ++i) { o.f[i] = a[i]; o.f[4 + i] = b[i]; }
     return o;
+}
+static __device__ __forceinline__ Vec8 from_f32(const float *p)
+{
+    return from_f32x4(reinterpret_cast<const f32x4_t *>(p)[0], reinterpret_cast<const f32x4_t *>(p)[1]);
 }
 // 8 values from element `at` (a multiple of 8) on, of either type
 template <bool F32>
@@ -188,13 +191,15 @@ static __device__ __forceinline__ Vec8 widen_raw(const u32x4_t (&r)[F32 ? 2 : 1]
 // second of what the first gives, so the next row is loaded before the first: its way from memory is then behind both. What a
 // thread past the row's end loads is the row's first vector, and nothing comes of it.
 template <int TPR, int V, bool F32>
-__global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), 4) void residual_norm_backward_kernel(NormLaunch a)
+__global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), (V == 1 ? 4 : 2)) void residual_norm_backward_kernel(NormLaunch a)
 {
     typedef RowCfg<TPR, V> R;
     constexpr int ROWS = R::ROWS;
-    // One vector a thread: the parameters stay in 128 registers, and the next row is loaded early. Two: neither has room, and a row is
-    // loaded again where it is used again.
+    // One vector a thread: the parameters stay in 128 registers, and the next row is loaded early. Two: neither has room, and of
+    // the three partial sums two lie in LDS ([2][V][2][TPR] four floats each; with all three in registers 16384 values a row
+    // spilled and reached 2.0 TB/s).
     constexpr bool KEEP = V == 1;
+    extern __shared__ f32x4_t s_acc[];
     __shared__ float s_a[2][3 * 16], s_b[2][16];      // in turns, so that a row's places are not those a slower wavefront still reads
     const int lane = R::lane(), chunk = blockIdx.x * ROWS + R::row();
     if (TPR == 64 && chunk >= a.chunks) return;
@@ -216,14 +221,44 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), 4) void residual_norm_ba
         there[v] = in ? 1.0f : 0.0f;
     }
     const bool has_dh = a.dh != nullptr, has_dy = a.dy != nullptr, has_b = a.block != nullptr, post = a.post != nullptr, gated = a.gate != nullptr;
-    Vec8 dpost[V], dgate[V], dpre[V], w[V], p[V], gt[V];
+    Vec8 kept_post{}, dgate[V], kept_pre{}, kept_w{}, kept_p{}, kept_g{};
 #pragma unroll
-    for (int v = 0; v < V; ++v) dpost[v] = dgate[v] = dpre[v] = w[v] = p[v] = gt[v] = Vec8{};
-    auto params = [&](int v) __attribute__((always_inline)) {
-        if (has_dh) w[v] = param8(a.pre, a.param_f32, col[v]);
-        if (post) p[v] = param8(a.post, a.param_f32, col[v]);
+    for (int v = 0; v < V; ++v) dgate[v] = Vec8{};
+    auto place = [&](int which, int v, int half) __attribute__((always_inline)) { return s_acc + ((which * V + v) * 2 + half) * TPR + lane; };
+    if constexpr (!KEEP)
+#pragma unroll
+        for (int k = 0; k < 4 * V; ++k) s_acc[k * TPR + lane] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // sum += t, of dpost (which = 0) or dpre (1): only this thread uses its places
+    auto add = [&](Vec8 &kept, int which, int v, const Vec8 &t) __attribute__((always_inline)) {
+        if constexpr (KEEP) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) kept.f[e] += t.f[e];
+        } else {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                f32x4_t s4 = *place(which, v, half);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s4[e] += t.f[4 * half + e];
+                *place(which, v, half) = s4;
+            }
+        }
     };
-    if constexpr (KEEP) params(0);
+    auto total = [&](const Vec8 &kept, int which, int v) __attribute__((always_inline)) {
+        if constexpr (KEEP) return kept;
+        else return from_f32x4(*place(which, v, 0), *place(which, v, 1));
+    };
+    if constexpr (KEEP) {
+        if (has_dh) kept_w = param8(a.pre, a.param_f32, col[0]);
+        if (post) kept_p = param8(a.post, a.param_f32, col[0]);
+    }
+    auto param = [&](const Vec8 &kept, const void *from, int64_t at) __attribute__((always_inline)) {
+        if constexpr (KEEP) return kept;
+        else return from ? param8(from, a.param_f32, at) : Vec8{};
+    };
+    // without KEEP: one vector's values at a time
+    auto apart = [&]() __attribute__((always_inline)) {
+        if constexpr (!KEEP) __builtin_amdgcn_sched_barrier(0);
+    };
     auto load = [&](RawRow<F32> &raw, int64_t row, int v) __attribute__((always_inline)) {
         const int64_t at = row * a.width + col[v];
         if (has_dh) {
@@ -240,27 +275,32 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), 4) void residual_norm_ba
     for (int64_t row = begin; row < end; ++row) {
         const int64_t at = row * a.width;
         const int parity = (int)(row - begin) & 1;
-        RawRow<F32> now = next;
+        RawRow<F32> now[V];
+        if constexpr (KEEP) now[0] = next;
+        else
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                now[v] = RawRow<F32>{};
+                load(now[v], row, v);
+            }
         Vec8 d[V];                         // dy, then dY, then post * dn
         float s[3] = {0.f, 0.f, 0.f};      // y^2, u y, b^2
-        if (KEEP && gated && new_gate) gt[0] = param8(a.gate, a.param_f32, (int64_t)group * a.width + col[0]);
+        if (KEEP && gated && new_gate) kept_g = param8(a.gate, a.param_f32, (int64_t)group * a.width + col[0]);
         new_gate = false;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            if constexpr (!KEEP) {
-                params(v);
-                load(now, row, v);
-            }
-            const Vec8 y = widen_raw<F32>(now.y), b = widen(now.b), dh = widen(now.dh);
+            const Vec8 w = param(kept_w, has_dh ? a.pre : nullptr, col[v]);
+            const Vec8 y = widen_raw<F32>(now[v].y), b = widen(now[v].b), dh = widen(now[v].dh);
             float t[3] = {0.f, 0.f, 0.f};
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 t[0] = fmaf(y.f[e], y.f[e], t[0]);
-                t[1] = fmaf(w[v].f[e] * dh.f[e], y.f[e], t[1]);
+                t[1] = fmaf(w.f[e] * dh.f[e], y.f[e], t[1]);
                 t[2] = fmaf(b.f[e], b.f[e], t[2]);
             }
 #pragma unroll
             for (int k = 0; k < 3; ++k) s[k] += there[v] != 0.f ? t[k] : 0.f;
+            apart();
         }
         if (KEEP && row + 1 < end) load(next, row + 1, 0);
         thread_sums<TPR, 3>(s, s_a[parity]);
@@ -270,20 +310,19 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), 4) void residual_norm_ba
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const bool in = there[v] != 0.f;
-            if constexpr (!KEEP) {
-                params(v);
-                if (gated) gt[v] = param8(a.gate, a.param_f32, (int64_t)group * a.width + col[v]);
-                load(now, row, v);
-            }
-            d[v] = widen_raw<F32>(now.dy);
-            const Vec8 b = widen(now.b);
+            const Vec8 w = param(kept_w, has_dh ? a.pre : nullptr, col[v]), p = param(kept_p, a.post, col[v]);
+            const Vec8 gt = param(kept_g, a.gate, (int64_t)group * a.width + col[v]);
+            d[v] = widen_raw<F32>(now[v].dy);
+            const Vec8 b = widen(now[v].b);
             if (has_dh) {
-                const Vec8 y = widen_raw<F32>(now.y), dh = widen(now.dh);
+                const Vec8 y = widen_raw<F32>(now[v].y), dh = widen(now[v].dh);
+                Vec8 t;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    d[v].f[e] += fmaf(r * w[v].f[e], dh.f[e], -y.f[e] * back);
-                    dpre[v].f[e] = fmaf(dh.f[e] * r, y.f[e], dpre[v].f[e]);
+                    d[v].f[e] += fmaf(r * w.f[e], dh.f[e], -y.f[e] * back);
+                    t.f[e] = dh.f[e] * r * y.f[e];
                 }
+                add(kept_pre, 1, v, t);
             }
             if (a.y && in) {
                 Vec8 o;
@@ -294,21 +333,24 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), 4) void residual_norm_ba
             if (gated) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float n = post ? b.f[e] * rb * p[v].f[e] : b.f[e];
+                    const float n = post ? b.f[e] * rb * p.f[e] : b.f[e];
                     dgate[v].f[e] = fmaf(d[v].f[e], n, dgate[v].f[e]);
-                    d[v].f[e] *= gt[v].f[e];
+                    d[v].f[e] *= gt.f[e];
                 }
             }
             if (post) {
-                float t = 0.f;
+                float sum = 0.f;
+                Vec8 t;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    dpost[v].f[e] = fmaf(d[v].f[e], b.f[e] * rb, dpost[v].f[e]);
-                    d[v].f[e] *= p[v].f[e];
-                    t = fmaf(d[v].f[e], b.f[e], t);
+                    t.f[e] = d[v].f[e] * (b.f[e] * rb);
+                    d[v].f[e] *= p.f[e];
+                    sum = fmaf(d[v].f[e], b.f[e], sum);
                 }
-                s4[0] += in ? t : 0.f;
+                s4[0] += in ? sum : 0.f;
+                add(kept_post, 0, v, t);
             }
+            apart();
         }
         if (post) thread_sums<TPR, 1>(s4, s_b[parity]);
         if (a.h) {
@@ -316,12 +358,12 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), 4) void residual_norm_ba
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 if (post) {
-                    if constexpr (!KEEP) now.b = *reinterpret_cast<const u32x4_t *>(a.block + at + col[v]);
-                    const Vec8 b = widen(now.b);
+                    const Vec8 b = widen(now[v].b);
 #pragma unroll
                     for (int e = 0; e < 8; ++e) d[v].f[e] = fmaf(rb, d[v].f[e], -b.f[e] * back_b);
                 }
                 if (there[v] != 0.f) store8<false>(a.h, at + col[v], d[v]);
+                apart();
             }
         }
         if (row + 1 == group_end && a.gate_rows) {
@@ -342,9 +384,9 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), 4) void residual_norm_ba
     for (int v = 0; v < V; ++v) {
         if (there[v] != 0.f) {
             const int64_t plane = (int64_t)a.chunks * a.width, at = (int64_t)chunk * a.width + col[v];
-            if (a.want_post) store8<true>(a.sums, at, dpost[v]);
+            if (a.want_post) store8<true>(a.sums, at, total(kept_post, 0, v));
             if (a.want_gate && !a.dgate) store8<true>(a.sums, plane + at, dgate[v]);
-            if (a.want_pre) store8<true>(a.sums, 2 * plane + at, dpre[v]);
+            if (a.want_pre) store8<true>(a.sums, 2 * plane + at, total(kept_pre, 1, v));
         }
     }
 }
@@ -392,8 +434,8 @@ int checked(const ficco_residual_norm_t *op, ficco_residual_norm_t *out)
     return FICCO_OK;
 }
 
-// Threads a row in the backward: one vector a thread, as far as a workgroup's 1024 threads go.
-int backward_tpr(int64_t width)
+// Threads a row: one vector a thread, as far as a workgroup's 1024 threads go.
+int threads_of(int64_t width)
 {
     for (int tpr : {64, 128, 192, 256, 384, 512, 768})
         if (width <= tpr * 8) return tpr;
@@ -407,7 +449,7 @@ struct Chunks {
 Chunks chunks_of(const ficco_residual_norm_t &o)
 {
     // as many as run at once on 256 CUs with 1024 threads each; but a chunk's sums are written and read again, so at least four rows
-    const int64_t target = 256 * 1024 / backward_tpr(o.width);
+    const int64_t target = 256 * 1024 / threads_of(o.width);
     const int64_t each = std::max<int64_t>(4, (o.rows + target - 1) / target);
     Chunks c{};
     if (!o.gate_rows || o.gate_rows >= o.rows) {
@@ -441,12 +483,16 @@ int launch_forward_t(const NormLaunch &a, bool f32, hipStream_t s)
 
 int launch_forward(const NormLaunch &a, bool f32, hipStream_t s)
 {
-    if (a.width <= 512) return launch_forward_t<64, 1>(a, f32, s);
-    if (a.width <= 1024) return launch_forward_t<64, 2>(a, f32, s);
-    if (a.width <= 2048) return launch_forward_t<256, 1>(a, f32, s);
-    if (a.width <= 4096) return launch_forward_t<256, 2>(a, f32, s);
-    if (a.width <= 8192) return launch_forward_t<256, 4>(a, f32, s);
-    return launch_forward_t<512, 4>(a, f32, s);
+    switch (threads_of(a.width)) {
+    case 64: return launch_forward_t<64, 1>(a, f32, s);
+    case 128: return launch_forward_t<128, 1>(a, f32, s);
+    case 192: return launch_forward_t<192, 1>(a, f32, s);
+    case 256: return launch_forward_t<256, 1>(a, f32, s);
+    case 384: return launch_forward_t<384, 1>(a, f32, s);
+    case 512: return launch_forward_t<512, 1>(a, f32, s);
+    case 768: return launch_forward_t<768, 1>(a, f32, s);
+    }
+    return a.width <= 8192 ? launch_forward_t<1024, 1>(a, f32, s) : launch_forward_t<1024, 2>(a, f32, s);
 }
 
 template <int TPR, int V>
@@ -454,15 +500,17 @@ int launch_backward_t(const NormLaunch &a, bool f32, hipStream_t s)
 {
     typedef RowCfg<TPR, V> R;
     const dim3 grid((unsigned)((a.chunks + R::ROWS - 1) / R::ROWS)), block(R::THREADS);
-    if (f32) hipLaunchKernelGGL((residual_norm_backward_kernel<TPR, V, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((residual_norm_backward_kernel<TPR, V, false>), grid, block, 0, s, a);
+    constexpr int LDS = V == 1 ? 0 : 2 * V * 2 * TPR * 16;
+    const auto fn = f32 ? &residual_norm_backward_kernel<TPR, V, true> : &residual_norm_backward_kernel<TPR, V, false>;
+    if (LDS) HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+    hipLaunchKernelGGL(fn, grid, block, LDS, s, a);
     HIP_TRY(hipGetLastError());
     return FICCO_OK;
 }
 
 int launch_backward(const NormLaunch &a, bool f32, hipStream_t s)
 {
-    switch (backward_tpr(a.width)) {
+    switch (threads_of(a.width)) {
     case 64: return launch_backward_t<64, 1>(a, f32, s);
     case 128: return launch_backward_t<128, 1>(a, f32, s);
     case 192: return launch_backward_t<192, 1>(a, f32, s);
