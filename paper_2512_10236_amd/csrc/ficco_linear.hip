@@ -105,97 +105,111 @@ int tile_for(int64_t M, int64_t K, int64_t N, double *us)
 }
 
 // ------------------------------------------------------------------------------------------------------------ few rows
-// A product of a few rows is the weight's way through the chip, once, and where that is short, the latency of one load and of
-// one join. A workgroup has a tile of 16 FM rows x 16 NB columns and all of k, its 8 wavefronts every 8th k-tile (128 bytes of a row) each, so that
-// together they read 1 KiB of each row at a time: fragments come
-// straight from memory into registers (both operands have k contiguous, nothing is shared between wavefronts), U k-tiles
-// at a time, the next U on their way while these are multiplied; the eight partial tiles are added through LDS, in the order
-// of the wavefronts. So narrow tiles over all of k, instead of wide ones, spread the weight over as many CUs as there are.
-template <int FM_, int NB_>
+// A product of a few rows is the weight's way through the chip, once, and where that is short, the latency of a load and of a
+// join. A workgroup has a tile of 8 AB rows x 16 NB columns and all of k, its 8 wavefronts every 8th k-tile each (128 bytes of a
+// row, so that together they read 1 KiB of each row at a time). A wavefront streams its k-tiles through a ring of D stages of its
+// own in LDS, without barriers: a stage is filled by loads of 8 rows x 128 bytes straight to LDS, which is what makes whole lines
+// of them, and read as fragments. The eight partial tiles are added through LDS in the order of the wavefronts. So narrow tiles
+// over all of k, instead of wide ones, spread the weight over as many CUs as there are.
+// Fragments loaded from memory directly, a lane a row: a CU then draws 16 bytes a cycle, one lane's at a time.
+template <int AB_, int NB_>
 struct RowsCfg {
-    static constexpr int FM = FM_, NB = NB_, WAVES = 8, U = FM + NB <= 2 ? 4 : FM + NB <= 3 ? 2 : 1;
+    static constexpr int AB = AB_, NB = NB_, WAVES = 8, FM = AB < 2 ? 1 : AB / 2, BM = 8 * AB, BN = 16 * NB;
+    static constexpr int LOADS = AB + 2 * NB, STAGE = LOADS * 1024;              // a wavefront's, per k-tile
+    static constexpr int D = 160 * 1024 / (WAVES * STAGE) < 6 ? 160 * 1024 / (WAVES * STAGE) : 6;
+    static constexpr int RING = D * STAGE, PART = FM * NB * 1024;
+    static constexpr int LDS_BYTES = WAVES * (RING > PART ? RING : PART);
+    static_assert(D >= 2 && (D - 1) * LOADS < 64, "a ring of two stages or more, vmcnt has 6 bits");
 };
 constexpr int kRowsThreads = 512;
 
 template <class T>
 __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch a)
 {
-    __shared__ f32x4_t s_part[T::WAVES][T::FM * T::NB][64];
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), j = lane & 15, g = lane >> 4;
     // tiles in 8 runs, one per XCD, rows fastest: the row tiles that read the same columns of the weight share an L2
-    const int tiles_m = (a.M + 16 * T::FM - 1) / (16 * T::FM), tiles_n = (a.N + 16 * T::NB - 1) / (16 * T::NB);
+    const int tiles_m = (a.M + T::BM - 1) / T::BM, tiles_n = (a.N + T::BN - 1) / T::BN;
     const XcdRun run = xcd_run(blockIdx.x, gridDim.x, tiles_m * tiles_n);
     const int lid = run.start + run.first;
-    const int row0 = lid % tiles_m * 16 * T::FM, col0 = lid / tiles_m * 16 * T::NB;
-    const int pairs = a.K / kBK;               // k-tiles: the wavefront has every 8th
-    const uint16_t *pa[T::FM], *pw[T::NB];                     // rows and columns that are not there: the last that is
+    const int row0 = lid % tiles_m * T::BM, col0 = lid / tiles_m * T::BN;
+    const int KT = scalar(a.K) / kBK;
+    const uint16_t *const A = scalar_base(a.A + (int64_t)row0 * a.lda), *const W = scalar_base(a.Wt + (int64_t)col0 * a.K);
+    const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * T::RING;
+    // 16-byte slot c of row r of 16 lies at slot c ^ ((r >> 1) & 7); rows and columns that are not there: the last that is
+    uint32_t off[T::LOADS];
 #pragma unroll
-    for (int i = 0; i < T::FM; ++i) pa[i] = a.A + (int64_t)min(row0 + 16 * i + j, a.M - 1) * a.lda + g * 8;
-#pragma unroll
-    for (int n = 0; n < T::NB; ++n) pw[n] = a.Wt + (int64_t)min(col0 + 16 * n + j, a.N - 1) * a.K + g * 8;
+    for (int l = 0; l < T::LOADS; ++l) {
+        const int r = (l < T::AB ? l : l - T::AB) * 8 + lane / 8;
+        const int row = l < T::AB ? min(r, a.M - 1 - row0) : min(r, a.N - 1 - col0);
+        off[l] = ((uint32_t)row * (uint32_t)(l < T::AB ? a.lda : a.K) + (uint32_t)(((lane % 8) ^ ((r >> 1) & 7)) * 8)) * 2u;
+    }
+    auto issue = [&](int kt, uint32_t stage) __attribute__((always_inline)) {
+        static_for<T::LOADS>([&](auto l_c) __attribute__((always_inline)) {
+            constexpr int l = decltype(l_c)::value;
+            set_lds_target<l * 1024>(ring + stage);
+            asm volatile("s_nop 0" ::: "memory");
+            load_to_lds_16((l < T::AB ? A : W) + (int64_t)kt * kBK, off[l]);
+        });
+        __builtin_amdgcn_sched_barrier(0);
+    };
     f32x4_t acc[T::FM][T::NB];
 #pragma unroll
     for (int i = 0; i < T::FM; ++i)
 #pragma unroll
         for (int n = 0; n < T::NB; ++n) acc[i][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    struct Frags {
-        bf16x8_t a[T::U][2][T::FM], w[T::U][2][T::NB];
-    } f0, f1;
-    auto load = [&](Frags &f, int p0) __attribute__((always_inline)) {
+    if (wave < KT) {
+        // past the wavefront's last k-tile the loads go on, on that k-tile again and into stages that are not read
+        const int last = wave + (KT - 1 - wave) / T::WAVES * T::WAVES;
 #pragma unroll
-        for (int u = 0; u < T::U; ++u) {
-            const int64_t k = (int64_t)min(p0 + u * T::WAVES, pairs - 1) * kBK;
+        for (int d = 0; d < T::D; ++d) issue(min(wave + d * T::WAVES, last), d * T::STAGE);
+        uint32_t stage = 0;
+#pragma clang loop unroll(disable)
+        for (int kt = wave; kt < KT; kt += T::WAVES) {
+            wait_vmem<(T::D - 1) * T::LOADS>();
+            __builtin_amdgcn_sched_barrier(0);
+            const unsigned char *const base = smem + wave * T::RING + stage;
+            bf16x8_t fa[2][T::FM], fw[2][T::NB];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
+                const int slot = ((4 * h + g) ^ ((j >> 1) & 7)) << 4;
 #pragma unroll
-                for (int n = 0; n < T::NB; ++n) f.w[u][h][n] = *reinterpret_cast<const bf16x8_t *>(pw[n] + k + 32 * h);
+                for (int i = 0; i < T::FM; ++i) fa[h][i] = *reinterpret_cast<const bf16x8_t *>(base + (16 * i + (T::AB == 1 ? j & 7 : j)) * 128 + (T::AB == 1 ? ((4 * h + g) ^ (((j & 7) >> 1) & 7)) << 4 : slot));
 #pragma unroll
-                for (int i = 0; i < T::FM; ++i) f.a[u][h][i] = *reinterpret_cast<const bf16x8_t *>(pa[i] + k + 32 * h);
+                for (int n = 0; n < T::NB; ++n) fw[h][n] = *reinterpret_cast<const bf16x8_t *>(base + T::AB * 1024 + (16 * n + j) * 128 + slot);
             }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the stage has been read: it may be filled again
+            __builtin_amdgcn_sched_barrier(0);
+            issue(min(kt + T::D * T::WAVES, last), stage);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+                    for (int n = 0; n < T::NB; ++n) acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[h][n], fa[h][i], acc[i][n], 0, 0, 0);
+            stage = stage == (T::D - 1) * T::STAGE ? 0 : stage + T::STAGE;
         }
-    };
-    auto multiply = [&](const Frags &f, int p0) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < T::U; ++u)
-            if (p0 + u * T::WAVES < pairs) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < T::FM; ++i)
-#pragma unroll
-                        for (int n = 0; n < T::NB; ++n)
-                            acc[i][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.w[u][h][n], f.a[u][h][i], acc[i][n], 0, 0, 0);
-            }
-    };
-    constexpr int STEP = T::U * T::WAVES;
-    if (wave < pairs) {
-        load(f0, wave);
-        for (int p = wave;;) {
-            if (p + STEP < pairs) load(f1, p + STEP);
-            multiply(f0, p);
-            if ((p += STEP) >= pairs) break;
-            if (p + STEP < pairs) load(f0, p + STEP);
-            multiply(f1, p);
-            if ((p += STEP) >= pairs) break;
-        }
+        wait_vmem<0>();                    // no load may arrive in LDS that is used for something else
     }
+    __syncthreads();
+    f32x4_t *const part = reinterpret_cast<f32x4_t *>(smem);
 #pragma unroll
     for (int i = 0; i < T::FM; ++i)
 #pragma unroll
-        for (int n = 0; n < T::NB; ++n) s_part[wave][i * T::NB + n][lane] = acc[i][n];
+        for (int n = 0; n < T::NB; ++n) part[(wave * T::FM * T::NB + i * T::NB + n) * 64 + lane] = acc[i][n];
     __syncthreads();
     for (int q = wave; q < T::FM * T::NB; q += T::WAVES) {
-        f32x4_t z = s_part[0][q][lane];
+        f32x4_t z = part[q * 64 + lane];
 #pragma unroll
         for (int w = 1; w < T::WAVES; ++w) {
-            const f32x4_t t = s_part[w][q][lane];
+            const f32x4_t t = part[(w * T::FM * T::NB + q) * 64 + lane];
 #pragma unroll
             for (int v = 0; v < 4; ++v) z[v] += t[v];
         }
         // z[v] is C[row0 + 16 i + lane % 16][col0 + 16 n + 4 (lane / 16) + v]; N is a multiple of 8
         const int64_t m = row0 + 16 * (q / T::NB) + j;
         const int n = col0 + 16 * (q % T::NB) + 4 * g;
-        if (m < a.M && n < a.N) {
+        if (m < min(a.M, row0 + T::BM) && n < a.N) {
             const f32x4_t bias = bias4(a.e, n);
             with_activation(a.e.activation, [&](auto act) __attribute__((always_inline)) { store4<act.value>(a.e, z, bias, a.C + m * a.ldc + n, m, n); });
         }
@@ -205,41 +219,53 @@ __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch 
 template <class T>
 int launch_rows_t(const LinearLaunch &a, hipStream_t s)
 {
-    const int64_t tiles = ((a.M + 16 * T::FM - 1) / (16 * T::FM)) * (((int64_t)a.N + 16 * T::NB - 1) / (16 * T::NB));
+    const int64_t tiles = (((int64_t)a.M + T::BM - 1) / T::BM) * (((int64_t)a.N + T::BN - 1) / T::BN);
     if (tiles > 0x7FFFFFFF / kRowsThreads) return FICCO_ERR_SHAPE;
-    hipLaunchKernelGGL(linear_rows_kernel<T>, dim3((unsigned)tiles), dim3(kRowsThreads), 0, s, a);
+    static bool set[64];                   // per device
+    int dev = 0;
+    HIP_TRY(hipGetDevice(&dev));
+    if (dev >= 64 || !set[dev]) {
+        HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(&linear_rows_kernel<T>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES));
+        if (dev < 64) set[dev] = true;
+    }
+    hipLaunchKernelGGL(linear_rows_kernel<T>, dim3((unsigned)tiles), dim3(kRowsThreads), T::LDS_BYTES, s, a);
     HIP_TRY(hipGetLastError());
     return FICCO_OK;
 }
 
-// Tiles of the few-rows kernel: 16 fm rows x 16 nb columns
-#define FICCO_FOR_EACH_ROWS(X) X(1, 1) X(1, 2) X(1, 4) X(2, 1) X(2, 2) X(4, 1)
-int launch_rows(int fm, int nb, const LinearLaunch &a, hipStream_t s)
+// Tiles of the few-rows kernel: 8 ab rows x 16 nb columns
+#define FICCO_FOR_EACH_ROWS(X) X(1, 1) X(1, 2) X(1, 4) X(2, 1) X(2, 2) X(2, 4) X(4, 1) X(4, 2) X(8, 1)
+int launch_rows(int ab, int nb, const LinearLaunch &a, hipStream_t s)
 {
-#define X(FM, NB) if (fm == FM && nb == NB) return launch_rows_t<RowsCfg<FM, NB>>(a, s);
+#define X(AB, NB) if (ab == AB && nb == NB) return launch_rows_t<RowsCfg<AB, NB>>(a, s);
     FICCO_FOR_EACH_ROWS(X)
 #undef X
     return FICCO_ERR_ARG;
 }
 
-// The few-rows kernel's tile, if it is expected to be faster than the other kernels' estimate (us); fm = 0: it is not. A round of
-// its tiles takes what a CU draws, about 110 KB a us, of its rows and columns over all of k; a launch cannot be faster than the
-// weight's way from memory.
+// The few-rows kernel's tile, if it is expected to be faster than the other kernels' estimate (us); ab = 0: it is not. A CU draws the
+// tile's rows and columns over all of k, at 146 KB a us alone and 90 when all do; a round of tiles more costs 2.5 us, since a
+// CU holds one workgroup; and a launch cannot be faster than the weight's way through the chip, 7.3 TB/s if it is cached.
+// Fitted to M 1-256 of eight shapes, K 512-16384, N 64-14336, each tile forced in turn (us, the other kernels / the tile taken:
+// M 16, K 8192, N 3584 29.6 / 11.6; M 64 29.9 / 14.9; M 128 29.7 / 25.5; M 256 32.3, its best tile 48.9; M 64, K 4096, N 768 11.8 /
+// 5.5; M 16, K 8192, N 64 18.8 / 5.9; M 64, K 4096, N 14336 21.6, its best tile 32.3).
 struct RowsTile {
-    int fm, nb;
+    int ab, nb;
 };
 RowsTile rows_tile(int64_t M, int64_t K, int64_t N, double us)
 {
     RowsTile best{0, 0};
     if (M > 256) return best;
     const int cus = compute_units();
-#define X(FM, NB)                                                                                                                        \
-    {                                                                                                                                    \
-        const int64_t tm = (M + 16 * FM - 1) / (16 * FM), tn = (N + 16 * NB - 1) / (16 * NB), rounds = (tm * tn + cus - 1) / cus;        \
-        const double drawn = (double)rounds * (16 * NB + (double)std::min<int64_t>(M, 16 * FM)) * (double)K * 2.0 / 110e3;               \
-        const double t = 2.5 + std::max(drawn, (double)(N * K + M * K) * 2.0 / 4.9e6);                                                   \
-        if ((FM == 1 || M > 16 * FM / 2) && t < us) { us = t; best = {FM, NB}; }                                                         \
-    }
+    auto consider = [&](int ab, int nb) {
+        if (ab > 1 && M <= 8 * ab / 2) return;                 // half of the rows or more would not be there
+        const int64_t tiles = ((M + 8 * ab - 1) / (8 * ab)) * ((N + 16 * nb - 1) / (16 * nb)), full = tiles / cus, rest = tiles - full * cus;
+        const double kb = (16 * nb + 8 * ab) * (double)K * 2e-3;
+        const double drawn = (double)full * kb / 90 + (rest ? kb / (146.0 - 56.0 * (double)rest / cus) : 0) + 2.5 * (double)((tiles + cus - 1) / cus - 1);
+        const double t = 3.0 + std::max(drawn, (double)(N * K + M * K) * 2 / 7.3e6);
+        if (t < us * 0.999) { us = t; best = {ab, nb}; }
+    };
+#define X(AB, NB) consider(AB, NB);
     FICCO_FOR_EACH_ROWS(X)
 #undef X
     return best;
@@ -531,7 +557,7 @@ int forward(const ficco_linear_t *op, const void *A, const void *W, const void *
         wt = (const uint16_t *)workspace;
     }
     const LinearLaunch a{(const uint16_t *)A, wt, (uint16_t *)C, o.lda, o.ldc, (int32_t)o.M, (int32_t)o.N, (int32_t)o.K, 0, e};
-    return f.rows.fm ? launch_rows(f.rows.fm, f.rows.nb, a, s) : launch_tiles(f.tile, a, s);
+    return f.rows.ab ? launch_rows(f.rows.ab, f.rows.nb, a, s) : launch_tiles(f.tile, a, s);
 }
 
 int backward(const ficco_linear_t *op, const void *A, const void *W, const void *pre, const void *dC, void *dA, void *dW, void *dbias, void *workspace,
