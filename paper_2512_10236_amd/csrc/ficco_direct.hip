@@ -20,9 +20,7 @@
 namespace ficco {
 namespace {
 
-typedef short i16x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
-typedef __attribute__((address_space(3))) i16x4_t lds_i16x4_t;
 
 // A stage is two halves of 64 k values, a half 16 FM rows of A (128 bytes each, k contiguous) and then 64 rows of W
 // (128 bytes each, 64 columns). 16-byte slots are swizzled: slot s of row r of A lies at s ^ ((r >> 1) & 7), as in the

@@ -56,4 +56,22 @@ static __device__ __forceinline__ void thread_sums(float (&v)[N], float *s)
     }
 }
 
+// Sum over k in [0, n) of in[k * stride] by a workgroup of 1024 threads: 32 columns side by side (`in` is the thread's, column threadIdx.x
+// % 32; there: it exists), 32 slices of k, joined through LDS (`s`: 32 x 32 floats) in the order of the slices. The first 32
+// threads have the sums.
+static __device__ __forceinline__ float column_sum(const float *in, int n, int64_t stride, bool there, float (*s)[32])
+{
+    const int col = threadIdx.x & 31, slice = threadIdx.x >> 5;
+    float t = 0.f;
+    if (there)
+#pragma unroll 8
+        for (int k = slice; k < n; k += 32) t += in[(int64_t)k * stride];
+    s[slice][col] = t;
+    __syncthreads();
+    if (slice) return 0.f;
+#pragma unroll
+    for (int k = 1; k < 32; ++k) t += s[k][col];
+    return t;
+}
+
 }  // namespace ficco

@@ -1,91 +1,21 @@
 // A product with bias, activation and residual in its epilogue, and its gradients (ficco_linear, ficco_linear_backward):
 //   z = A W + b,  C = act(z) + R          dZ = dC act'(z),  db = sum_m dZ,  dA = dZ W^T,  dW = A^T dZ
-// The products run on the tile routine of the GEMM kernels (ficco_tile.h): both operands with k contiguous, bf16 in, fp32
-// accumulators, k ascending. The epilogue takes the accumulators before they are rounded, so that bias, activation and
-// residual cost no pass over memory of their own.
+// The products run on the tile routine of the GEMM kernels (ficco_tile.h): bf16 in, fp32 accumulators, k ascending. The epilogue takes
+// the accumulators before they are rounded, so that bias, activation and residual cost no pass over memory of their own.
 //
 // The backward pass is bound by its two products. What they need beside their inputs is made once by turn_kernel, a streaming
-// kernel: dZ (with its column sums), and the operands with the other index contiguous.
-#include "ficco_operators.h"
-#include "ficco_epilogue.h"
+// kernel: dZ (with its column sums), and, where the products cannot read them as they are, the operands with the other index
+// contiguous.
+#include "ficco_linear.h"
+#include "ficco_lanes.h"
 
 namespace ficco {
 namespace {
 
-struct LinearLaunch {
-    const uint16_t *A, *Wt;       // [M,K] stride lda, [N,K] dense
-    uint16_t *C;
-    int64_t lda, ldc;
-    int32_t M, N, K, group_m;
-    Epilogue e;
-};
-
-// One launch over all tiles, at most as many workgroups as run at once; the tiles in the order of gemm_blocks_kernel.
-template <class T>
-__global__ __launch_bounds__(T::THREADS) void linear_tiles_kernel(LinearLaunch a)
-{
-    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
-    const int tiles_n = (a.N + T::BN - 1) / T::BN;
-    const int tiles_m = (int)(((int64_t)a.M + T::BM - 1) / T::BM);
-    const XcdRun run = xcd_run(blockIdx.x, gridDim.x, tiles_m * tiles_n);
-    const int per_group = a.group_m * tiles_n;
-    for (int t = run.first; t < run.count; t += run.stride) {
-        const int lid = run.start + t;
-        const int group = lid / per_group;
-        const int first_m = group * a.group_m;
-        const int gsz = min(tiles_m - first_m, a.group_m);
-        const int tm = first_m + (lid % per_group) % gsz;
-        const int tn = (lid % per_group) / gsz;
-        const int64_t row0 = (int64_t)tm * T::BM;
-        const int rows_valid = (int)min((int64_t)T::BM, a.M - row0);
-        const int col0 = tn * T::BN;
-        const int cols_valid = min(T::BN, a.N - col0);
-        TileAcc<T> ta;
-        tile_zero(ta);
-        tile_accumulate<T>(ta, a.A + row0 * a.lda, rows_valid, a.Wt + (int64_t)col0 * a.K, cols_valid, a.lda, a.K, a.K, smem);
-        with_activation(a.e.activation, [&](auto act) __attribute__((always_inline)) {
-            tile_store_epilogue<T, act.value>(ta, a.e, a.C + row0 * a.ldc + col0, rows_valid, cols_valid, a.ldc, row0, col0);
-        });
-        __syncthreads();                   // everyone is done with the ring before the next tile refills it
-    }
-    wait_vmem<0>();                        // no load may arrive in LDS that is not this workgroup's any more
-}
-
-template <class T>
-int launch_tiles_t(const LinearLaunch &a, hipStream_t s)
-{
-    const int64_t tiles_n = ((int64_t)a.N + T::BN - 1) / T::BN, tiles_m = ((int64_t)a.M + T::BM - 1) / T::BM, total = tiles_m * tiles_n;
-    if (total <= 0 || total > 0x7FFFFFFF || a.lda > kMaxK || a.K > kMaxK) return FICCO_ERR_SHAPE;
-    static int fit_of[64];                 // per device: workgroups that run at once, 0 = not asked yet
-    int dev = 0;
-    HIP_TRY(hipGetDevice(&dev));
-    int fit = dev < 64 ? fit_of[dev] : 0;
-    if (fit == 0) {
-        int per_cu = 0;
-        HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(&linear_tiles_kernel<T>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES));
-        HIP_TRY(hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, linear_tiles_kernel<T>, T::THREADS, T::LDS_BYTES));
-        fit = std::max(8, per_cu * compute_units() / 8 * 8);
-        if (dev < 64) fit_of[dev] = fit;
-    }
-    const int64_t grid = std::min<int64_t>(total, fit);
-    LinearLaunch b = a;
-    b.group_m = 8;
-    if (total > grid) {
-        double best = -1;
-        for (int g = 1; g <= 8; g *= 2) {
-            const double c = tile_order_cost(T::BM, T::BN, tiles_n, tiles_m, grid / 8, 1, g, (int64_t)a.M * a.K * 2, (int64_t)a.N * a.K * 2);
-            if (best < 0 || c < best) { best = c; b.group_m = g; }
-        }
-    }
-    hipLaunchKernelGGL(linear_tiles_kernel<T>, dim3((unsigned)grid), dim3(T::THREADS), T::LDS_BYTES, s, b);
-    HIP_TRY(hipGetLastError());
-    return FICCO_OK;
-}
-
 int launch_tiles(int tile, const LinearLaunch &a, hipStream_t s)
 {
     switch (tile) {
-#define X(id, T) case id: return launch_tiles_t<T>(a, s);
+#define X(id, T) case id: return launch_tiles_t<T, false, false>(a, s);
     FICCO_FOR_EACH_TILE(X)
 #undef X
     default: return FICCO_ERR_ARG;
@@ -134,7 +64,7 @@ __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch 
     const int lid = run.start + run.first;
     const int row0 = lid % tiles_m * T::BM, col0 = lid / tiles_m * T::BN;
     const int KT = scalar(a.K) / kBK;
-    const uint16_t *const A = scalar_base(a.A + (int64_t)row0 * a.lda), *const W = scalar_base(a.Wt + (int64_t)col0 * a.K);
+    const uint16_t *const A = scalar_base(a.A + (int64_t)row0 * a.lda), *const W = scalar_base(a.W + (int64_t)col0 * a.ldw);
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * T::RING;
     // 16-byte slot c of row r of 16 lies at slot c ^ ((r >> 1) & 7); rows and columns that are not there: the last that is
     uint32_t off[T::LOADS];
@@ -142,7 +72,7 @@ __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch 
     for (int l = 0; l < T::LOADS; ++l) {
         const int r = (l < T::AB ? l : l - T::AB) * 8 + lane / 8;
         const int row = l < T::AB ? min(r, a.M - 1 - row0) : min(r, a.N - 1 - col0);
-        off[l] = ((uint32_t)row * (uint32_t)(l < T::AB ? a.lda : a.K) + (uint32_t)(((lane % 8) ^ ((r >> 1) & 7)) * 8)) * 2u;
+        off[l] = ((uint32_t)row * (uint32_t)(l < T::AB ? a.lda : a.ldw) + (uint32_t)(((lane % 8) ^ ((r >> 1) & 7)) * 8)) * 2u;
     }
     auto issue = [&](int kt, uint32_t stage) __attribute__((always_inline)) {
         static_for<T::LOADS>([&](auto l_c) __attribute__((always_inline)) {
@@ -277,15 +207,20 @@ RowsTile rows_tile(int64_t M, int64_t K, int64_t N, double us)
 //   turned  [Cc][ldt], ldt = R rounded up to 64: src transposed, zero behind its end (null: not wanted)
 //   with z (stride ldz): the value is src * act'(z), rounded to bf16, instead of src
 //   same    [R][lds], lds = Cc rounded up to 64: the value in its own order, zero behind its end (null: not wanted)
-//   sums    [ceil(R/256)][Cc] fp32: column sums over 256 rows each, of the values before they are rounded (null: not wanted)
-// Streaming, bound by memory.
-struct TurnLaunch {
+//   sums    [ceil(R/64)][Cc] fp32: column sums over 64 rows each, of the values before they are rounded (null: not wanted)
+// Streaming, bound by memory: dZ of 8192 x 3584 in both orders 48 us, 4.9 TB/s. A workgroup is one wavefront, since small
+// operands are then spread over more CUs; up to three operands go in one launch, the first with z.
+struct TurnJob {
     const uint16_t *src, *z;
     uint16_t *turned, *same;
     float *sums;
     int64_t R, Cc, ld, ldz, ldt, lds;
 };
-constexpr int kTurnRows = 256;
+struct TurnLaunch {
+    TurnJob job[3];
+    int32_t first[3];             // number of each job's first workgroup
+};
+constexpr int kTurnRows = 64;
 
 // 16 bytes at `off` bytes from a uniform address, which stays in scalar registers
 static __device__ __forceinline__ u32x4_t load_at(const uint16_t *base, uint32_t off)
@@ -298,12 +233,12 @@ static __device__ __forceinline__ void store_at(uint16_t *base, uint32_t off, u3
 }
 
 template <int ACT>
-__global__ __launch_bounds__(256) void turn_kernel(TurnLaunch a)
+static __device__ __forceinline__ void turn_block(const TurnJob &a, int block)
 {
-    __shared__ float s_sum[4][64];
-    const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6);
+    const int lane = threadIdx.x;
     // the wavefront's place, and the lane's in it
-    const int64_t R0 = (int64_t)blockIdx.y * kTurnRows + wave * 64, C0 = (int64_t)blockIdx.x * 64;
+    const int tiles_c = (int)((a.Cc + 63) / 64), by = block / tiles_c;
+    const int64_t R0 = (int64_t)by * kTurnRows, C0 = (int64_t)(block - by * tiles_c) * 64;
     const int lr = (lane & 7) * 8, lc = (lane >> 3) * 8;
     const int rows = (int)min((int64_t)64, a.R - R0), cols = (int)min((int64_t)64, a.Cc - C0);     // of the wavefront's, that exist
     const bool in = lc < cols;
@@ -311,10 +246,7 @@ __global__ __launch_bounds__(256) void turn_kernel(TurnLaunch a)
     float sum[8];
 #pragma unroll
     for (int c = 0; c < 8; ++c) sum[c] = 0.f;
-    if (rows <= 0) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = u32x4_t{0u, 0u, 0u, 0u};
-    } else {
+    {
         // rows and columns that are not there are read at the last that is, and then put to zero: a load under a condition of
         // its own makes the compiler copy all the others
         const uint16_t *src = a.src + R0 * a.ld + C0;
@@ -376,24 +308,39 @@ __global__ __launch_bounds__(256) void turn_kernel(TurnLaunch a)
         }
     }
     if (a.sums) {
+        // over the 8 lanes of a column group
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
+        for (int c = 0; c < 8; ++c) sum[c] = lane_sum<8>(sum[c]);
+        float t = sum[0];
 #pragma unroll
-            for (int m = 1; m < 8; m <<= 1) sum[c] += __shfl_xor(sum[c], m, 64);
-        if ((lane & 7) == 0)
-#pragma unroll
-            for (int c = 0; c < 8; ++c) s_sum[wave][lc + c] = sum[c];
-        __syncthreads();
-        const int64_t c = C0 + threadIdx.x;
-        if (threadIdx.x < 64 && c < a.Cc)
-            a.sums[(int64_t)blockIdx.y * a.Cc + c] = (s_sum[0][threadIdx.x] + s_sum[1][threadIdx.x]) + (s_sum[2][threadIdx.x] + s_sum[3][threadIdx.x]);
+        for (int c = 1; c < 8; ++c) t = (lane & 7) == c ? sum[c] : t;
+        if (lane < cols) a.sums[(int64_t)by * a.Cc + C0 + lane] = t;
     }
 }
 
-int launch_turn(int activation, const TurnLaunch &a, hipStream_t s)
+template <int ACT>
+__global__ __launch_bounds__(64) void turn_kernel(TurnLaunch a)
 {
-    if (a.R < 1 || a.Cc < 8 || a.Cc % 8) return FICCO_ERR_SHAPE;
-    const dim3 grid((unsigned)((a.Cc + 63) / 64), (unsigned)((a.R + kTurnRows - 1) / kTurnRows)), block(256);
+    const int block = blockIdx.x;
+    if (block < a.first[1]) turn_block<ACT>(a.job[0], block);
+    else if (block < a.first[2]) turn_block<FICCO_ACT_NONE>(a.job[1], block - a.first[1]);
+    else turn_block<FICCO_ACT_NONE>(a.job[2], block - a.first[2]);
+}
+
+// Runs the jobs that have something to write, the first of them with the activation.
+int launch_turn(int activation, TurnLaunch a, hipStream_t s)
+{
+    int64_t blocks = 0;
+    for (int k = 0; k < 3; ++k) {
+        TurnJob &j = a.job[k];
+        a.first[k] = (int32_t)blocks;
+        if (!j.turned && !j.same && !j.sums) continue;
+        if (j.R < 1 || j.Cc < 8 || j.Cc % 8) return FICCO_ERR_SHAPE;
+        blocks += ((j.R + kTurnRows - 1) / kTurnRows) * ((j.Cc + 63) / 64);
+        if (blocks > 0x7FFFFFFF / 64) return FICCO_ERR_SHAPE;
+    }
+    if (!blocks) return FICCO_OK;
+    const dim3 grid((unsigned)blocks), block(64);
     switch (activation) {
     case FICCO_ACT_NONE: hipLaunchKernelGGL(turn_kernel<FICCO_ACT_NONE>, grid, block, 0, s, a); break;
     case FICCO_ACT_RELU: hipLaunchKernelGGL(turn_kernel<FICCO_ACT_RELU>, grid, block, 0, s, a); break;
@@ -406,23 +353,13 @@ int launch_turn(int activation, const TurnLaunch &a, hipStream_t s)
     return FICCO_OK;
 }
 
-// out[c] = sum over r of in[r][c], r in [0, R): 64 columns a workgroup, its 16 wavefronts take every 16th row. R = 0: zeros.
+// out[c] = sum over r of in[r][c], r in [0, R). R = 0: zeros.
 __global__ __launch_bounds__(1024) void sum_rows_kernel(const float *__restrict__ in, float *__restrict__ out, int R, int64_t Cc)
 {
-    __shared__ float s[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c = (int64_t)blockIdx.x * 64 + lane;
-    float t = 0.f;
-    if (c < Cc)
-#pragma unroll 4
-        for (int r = wave; r < R; r += 16) t += in[(int64_t)r * Cc + c];
-    s[wave][lane] = t;
-    __syncthreads();
-    if (wave == 0 && c < Cc) {
-#pragma unroll
-        for (int w = 1; w < 16; ++w) t += s[w][lane];
-        out[c] = t;
-    }
+    __shared__ float s[32][32];
+    const int64_t c = (int64_t)blockIdx.x * 32 + (threadIdx.x & 31);
+    const float t = column_sum(in + c, R, Cc, c < Cc, s);
+    if (threadIdx.x < 32 && c < Cc) out[c] = t;
 }
 
 __global__ __launch_bounds__(256) void zero_kernel(u32x4_t *p, int64_t vecs)
@@ -451,8 +388,8 @@ int checked(const ficco_linear_t *op, bool backward, ficco_linear_t *out)
     return FICCO_OK;
 }
 
-// How a forward goes: row blocks of the direct kernel, which takes a [K,N] weight as it is; or the few-rows kernel's tile for an [N,K]
-// one; or the others' tile.
+// How a forward goes: row blocks of the direct kernel, for a small product of a [K,N] weight; or the few-rows kernel's tile, for an
+// [N,K] one; or the tile of the others. These read a [K,N] weight as it is, but parts of tiles need it re-laid out.
 struct Forward {
     int row_blocks, tile;
     RowsTile rows;
@@ -466,16 +403,18 @@ Forward forward_way(const ficco_linear_t &o)
     f.tile = tile_for(o.M, o.K, o.N, &us);
     if (o.weight_layout == FICCO_WEIGHT_KN) {
         if (o.K * o.N * 2 <= 0x7FFFFFFF) f.row_blocks = direct_row_blocks(o.M, o.K, o.N, compute_units(), us);
-        if (!f.row_blocks) f.bytes = round_up(o.K * o.N * 2, 256);
+        if (!f.row_blocks && !strided_tile(f.tile, false)) f.bytes = round_up(o.K * o.N * 2, 256);
     } else {
         f.rows = rows_tile(o.M, o.K, o.N, us);
     }
     return f;
 }
 
-// The backward's workspace, in bytes from its start (-1: not needed).
+// How a backward goes: the tiles of the products that read their operands as they are (0: they are turned first), and the
+// workspace, in bytes from its start (-1: not needed).
 struct Backward {
     int64_t Mp, Np;               // M and N rounded up to whole k-tiles
+    int tile_a, tile_w;
     int64_t dz, dz_turned, a_turned, w_other, sums, bytes;
 };
 Backward backward_way(const ficco_linear_t &o)
@@ -484,6 +423,11 @@ Backward backward_way(const ficco_linear_t &o)
     b.Mp = round_up(o.M, kBK);
     b.Np = round_up(o.N, kBK);
     if (o.M == 0) return b;
+    const bool kn = o.weight_layout == FICCO_WEIGHT_KN;
+    // dA = dZ W^T sums over n, and an [N,K] weight has k next to each other; dW = A^T dZ sums over m, and A has k next to each other. What
+    // lies behind the last n or m must be zero, which only a copy is.
+    if (!kn && b.Np == o.N) b.tile_a = strided_tile(tile_for(o.M, b.Np, o.K, nullptr), false);
+    if (b.Mp == o.M) b.tile_w = strided_tile(tile_for(kn ? o.K : o.N, b.Mp, kn ? o.N : o.K, nullptr), kn);
     int64_t at = 0;
     auto take = [&](bool needed, int64_t bytes) {
         const int64_t here = at;
@@ -492,8 +436,8 @@ Backward backward_way(const ficco_linear_t &o)
     };
     b.dz = take(o.activation != FICCO_ACT_NONE || b.Np != o.N, o.M * b.Np * 2);
     b.dz_turned = take(true, o.N * b.Mp * 2);
-    b.a_turned = take(true, o.K * b.Mp * 2);
-    b.w_other = take(o.weight_layout == FICCO_WEIGHT_NK || b.Np != o.N, o.K * b.Np * 2);
+    b.a_turned = take(!b.tile_w, o.K * b.Mp * 2);
+    b.w_other = take(!b.tile_a && (!kn || b.Np != o.N), o.K * b.Np * 2);
     b.sums = take(true, (o.M + kTurnRows - 1) / kTurnRows * o.N * 4);
     b.bytes = at;
     return b;
@@ -515,6 +459,22 @@ int product(int64_t M, int64_t K, int64_t N, const uint16_t *A, int64_t lda, con
     HIP_TRY(launch_gemm(tile_for(M, K, N, nullptr), g, s));
     return FICCO_OK;
 }
+// The same with A as [K][M] or B as [K][N].
+int product_strided(int tile, bool a_strided, int64_t M, int64_t K, int64_t N, const uint16_t *A, int64_t lda, const uint16_t *B, int64_t ldb, uint16_t *C,
+                    hipStream_t s)
+{
+    LinearLaunch l{};
+    l.A = A;
+    l.W = B;
+    l.C = C;
+    l.lda = lda;
+    l.ldw = ldb;
+    l.ldc = N;
+    l.M = (int32_t)M;
+    l.N = (int32_t)N;
+    l.K = (int32_t)K;
+    return launch_tiles_strided(tile, a_strided, l, s);
+}
 
 int zero(void *p, int64_t bytes, hipStream_t s)
 {
@@ -525,7 +485,7 @@ int zero(void *p, int64_t bytes, hipStream_t s)
 
 int sum_rows(const float *in, float *out, int64_t R, int64_t Cc, hipStream_t s)
 {
-    hipLaunchKernelGGL(sum_rows_kernel, dim3((unsigned)((Cc + 63) / 64)), dim3(1024), 0, s, in, out, (int)R, Cc);
+    hipLaunchKernelGGL(sum_rows_kernel, dim3((unsigned)((Cc + 31) / 32)), dim3(1024), 0, s, in, out, (int)R, Cc);
     HIP_TRY(hipGetLastError());
     return FICCO_OK;
 }
@@ -551,13 +511,17 @@ int forward(const ficco_linear_t *op, const void *A, const void *W, const void *
         HIP_TRY(launch_direct_epilogue(f.row_blocks, d, e, o.lda, o.ldc, s));
         return FICCO_OK;
     }
-    const uint16_t *wt = (const uint16_t *)W;
+    LinearLaunch a{(const uint16_t *)A, (const uint16_t *)W, (uint16_t *)C, o.lda, o.K, o.ldc, (int32_t)o.M, (int32_t)o.N, (int32_t)o.K, 0, e};
+    if (f.rows.ab) return launch_rows(f.rows.ab, f.rows.nb, a, s);
     if (o.weight_layout == FICCO_WEIGHT_KN) {
+        if (!f.bytes) {
+            a.ldw = o.N;
+            return launch_tiles_strided(strided_tile(f.tile, false), false, a, s);
+        }
         HIP_TRY(launch_pack_weight((const uint16_t *)W, (uint16_t *)workspace, o.K, o.N, s));
-        wt = (const uint16_t *)workspace;
+        a.W = (const uint16_t *)workspace;
     }
-    const LinearLaunch a{(const uint16_t *)A, wt, (uint16_t *)C, o.lda, o.ldc, (int32_t)o.M, (int32_t)o.N, (int32_t)o.K, 0, e};
-    return f.rows.ab ? launch_rows(f.rows.ab, f.rows.nb, a, s) : launch_tiles(f.tile, a, s);
+    return launch_tiles(f.tile, a, s);
 }
 
 int backward(const ficco_linear_t *op, const void *A, const void *W, const void *pre, const void *dC, void *dA, void *dW, void *dbias, void *workspace,
@@ -582,38 +546,43 @@ int backward(const ficco_linear_t *op, const void *A, const void *W, const void 
     auto at = [&](int64_t off) { return off < 0 ? nullptr : (uint16_t *)(ws + off); };
     const bool kn = o.weight_layout == FICCO_WEIGHT_KN;
 
+    // dZ as the products need it, with its column sums; A with m contiguous; W with n contiguous
     TurnLaunch t{};
-    t.src = (const uint16_t *)dC;
-    t.z = (const uint16_t *)pre;
-    t.turned = dW ? at(b.dz_turned) : nullptr;
-    t.same = dA ? at(b.dz) : nullptr;
-    t.sums = dbias ? (float *)at(b.sums) : nullptr;
-    t.R = M; t.Cc = N; t.ld = o.ldc; t.ldz = o.ld_pre; t.ldt = b.Mp; t.lds = b.Np;
-    if (t.turned || t.same || t.sums)
-        if ((rc = launch_turn(o.activation, t, s))) return rc;
-    if (dbias && (rc = sum_rows((const float *)at(b.sums), (float *)dbias, (M + kTurnRows - 1) / kTurnRows, N, s))) return rc;
+    TurnJob &z = t.job[0], &ta = t.job[1], &tw = t.job[2];
+    z.src = (const uint16_t *)dC;
+    z.z = (const uint16_t *)pre;
+    z.turned = dW ? at(b.dz_turned) : nullptr;
+    z.same = dA ? at(b.dz) : nullptr;
+    z.sums = dbias ? (float *)at(b.sums) : nullptr;
+    z.R = M; z.Cc = N; z.ld = o.ldc; z.ldz = o.ld_pre; z.ldt = b.Mp; z.lds = b.Np;
+    if (dW && !b.tile_w) {
+        ta.src = (const uint16_t *)A;
+        ta.turned = at(b.a_turned);
+        ta.R = M; ta.Cc = K; ta.ld = o.lda; ta.ldt = b.Mp;
+    }
+    if (dA && b.w_other >= 0) {
+        tw.src = (const uint16_t *)W;
+        if (kn) { tw.same = at(b.w_other); tw.R = K; tw.Cc = N; tw.ld = N; tw.lds = b.Np; }
+        else { tw.turned = at(b.w_other); tw.R = N; tw.Cc = K; tw.ld = K; tw.ldt = b.Np; }
+    }
+    if ((rc = launch_turn(o.activation, t, s))) return rc;
+    if (dbias && (rc = sum_rows(z.sums, (float *)dbias, (M + kTurnRows - 1) / kTurnRows, N, s))) return rc;
+    const bool own = b.dz >= 0;
+    const uint16_t *const dz = own ? at(b.dz) : (const uint16_t *)dC;
+    const int64_t ldz = own ? b.Np : o.ldc;
     if (dA) {
-        // both operands with n contiguous: dZ, and W as [K,N]
-        const uint16_t *w = (const uint16_t *)W;
-        if (b.w_other >= 0) {
-            TurnLaunch u{};
-            u.src = (const uint16_t *)W;
-            if (kn) { u.R = K; u.Cc = N; u.ld = N; u.same = at(b.w_other); u.lds = b.Np; u.ldt = round_up(K, kBK); }
-            else { u.R = N; u.Cc = K; u.ld = K; u.turned = at(b.w_other); u.ldt = b.Np; u.lds = K; }
-            if ((rc = launch_turn(FICCO_ACT_NONE, u, s))) return rc;
-            w = at(b.w_other);
-        }
-        const bool own = b.dz >= 0;
-        if ((rc = product(M, b.Np, K, own ? at(b.dz) : (const uint16_t *)dC, own ? b.Np : o.ldc, w, (uint16_t *)dA, s))) return rc;
+        if (b.tile_a) rc = product_strided(b.tile_a, false, M, b.Np, K, dz, ldz, (const uint16_t *)W, K, (uint16_t *)dA, s);
+        else rc = product(M, b.Np, K, dz, ldz, b.w_other >= 0 ? at(b.w_other) : (const uint16_t *)W, (uint16_t *)dA, s);
+        if (rc) return rc;
     }
     if (dW) {
-        // both operands with m contiguous, in the order that gives dW W's layout
-        TurnLaunch u{};
-        u.src = (const uint16_t *)A;
-        u.R = M; u.Cc = K; u.ld = o.lda; u.turned = at(b.a_turned); u.ldt = b.Mp; u.lds = K;
-        if ((rc = launch_turn(FICCO_ACT_NONE, u, s))) return rc;
-        const uint16_t *first = at(kn ? b.a_turned : b.dz_turned), *second = at(kn ? b.dz_turned : b.a_turned);
-        if ((rc = product(kn ? K : N, b.Mp, kn ? N : K, first, b.Mp, second, (uint16_t *)dW, s))) return rc;
+        // in the order that gives dW W's layout
+        const uint16_t *const a = (const uint16_t *)A, *const zt = at(b.dz_turned);
+        if (b.tile_w && kn) rc = product_strided(b.tile_w, true, K, M, N, a, o.lda, zt, M, (uint16_t *)dW, s);
+        else if (b.tile_w) rc = product_strided(b.tile_w, false, N, M, K, zt, M, a, o.lda, (uint16_t *)dW, s);
+        else if (kn) rc = product(K, b.Mp, N, at(b.a_turned), b.Mp, zt, (uint16_t *)dW, s);
+        else rc = product(N, b.Mp, K, zt, b.Mp, at(b.a_turned), (uint16_t *)dW, s);
+        if (rc) return rc;
     }
     return FICCO_OK;
 }

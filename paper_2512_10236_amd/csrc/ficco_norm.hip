@@ -391,8 +391,8 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), (V == 1 ? 4 : 2)) void r
     }
 }
 
-// Sums of the chunks' partial sums, 64 columns a workgroup, 16 wavefronts taking every 16th chunk. blockIdx.y = 0: dpost over all
-// chunks, 1: dpre, 2 + g: dgate of group g over its own chunks.
+// Sums of the chunks' partial sums, 32 columns a workgroup. blockIdx.y = 0: dpost over all chunks, 1: dpre, 2 + g: dgate of group
+// g over its own chunks.
 struct SumLaunch {
     const float *sums;
     float *dpost, *dgate, *dpre;
@@ -400,25 +400,15 @@ struct SumLaunch {
 };
 __global__ __launch_bounds__(1024) void residual_norm_sum_kernel(SumLaunch a)
 {
-    __shared__ float s[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+    __shared__ float s[32][32];
+    const int c = blockIdx.x * 32 + (threadIdx.x & 31);
     const int64_t plane = (int64_t)a.chunks * a.width;
     const int y = blockIdx.y;
     const float *in = y == 0 ? a.sums : y == 1 ? a.sums + 2 * plane : a.sums + plane + (int64_t)(y - 2) * a.per_group * a.width;
     float *out = y == 0 ? a.dpost : y == 1 ? a.dpre : a.dgate ? a.dgate + (int64_t)(y - 2) * a.width : nullptr;
     if (!out) return;
-    const int n = y < 2 ? a.chunks : a.per_group;
-    float t = 0.f;
-    if (c < a.width)
-#pragma unroll 8
-        for (int k = wave; k < n; k += 16) t += in[(int64_t)k * a.width + c];
-    s[wave][lane] = t;
-    __syncthreads();
-    if (wave == 0 && c < a.width) {
-#pragma unroll
-        for (int w = 1; w < 16; ++w) t += s[w][lane];
-        out[c] = t;
-    }
+    const float t = column_sum(in + c, y < 2 ? a.chunks : a.per_group, a.width, c < a.width, s);
+    if (threadIdx.x < 32 && c < a.width) out[c] = t;
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -573,7 +563,7 @@ int backward(const ficco_residual_norm_t *op, const void *y, const void *block, 
         if ((rc = launch_backward(a, o.stream_type == FICCO_F32, s))) return rc;
     }
     if (dpost || dpre || t.dgate) {
-        hipLaunchKernelGGL(residual_norm_sum_kernel, dim3((unsigned)((o.width + 63) / 64), (unsigned)(2 + groups)), dim3(1024), 0, s, t);
+        hipLaunchKernelGGL(residual_norm_sum_kernel, dim3((unsigned)((o.width + 31) / 32), (unsigned)(2 + groups)), dim3(1024), 0, s, t);
         HIP_TRY(hipGetLastError());
     }
     return FICCO_OK;

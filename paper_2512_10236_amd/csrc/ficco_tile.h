@@ -171,6 +171,55 @@ struct SlicedA {
     __device__ __forceinline__ const uint16_t *at(int kt) const { return base + (int64_t)(kt - kt_begin) * T::BK; }
 };
 
+// How an operand lies in memory: a row's k values next to each other (KContiguous), or a k value's rows next to each other
+// (KStrided: the operand as [k][DIM], row stride ld, as the caller has it where the other layout would be a copy). A stage of the
+// latter is 64 rows of 2 DIM bytes, a fragment comes out of it by transposing reads (ds_read_b64_tr_b16: 16 lanes read 4 rows
+// x 16 columns, lane i gets column i; two of them make a fragment's 8 k values). 16-byte slot s of row r lies at s ^
+// strided_swizzle(r): half a wavefront's transposing read touches rows 0-3 and 8-11, 32 bytes each, which this spreads over all
+// 64 banks (rows that are multiples of 256 bytes need all 8 places of it, others differ by half of it already).
+struct KContiguous { static constexpr bool STRIDED = false; };
+struct KStrided { static constexpr bool STRIDED = true; };
+template <int DIM>
+static __device__ __forceinline__ int strided_swizzle(int row)
+{
+    static_assert(DIM % 64 == 0, "whole lines");
+    return DIM % 128 == 0 ? 2 * ((row & 3) | (((row >> 3) & 1) << 2)) : 2 * (((row >> 1) & 1) | (((row >> 3) & 1) << 1));
+}
+// Byte offset, from the tile's first column of its first row, of what lane `lane` fetches for 1 KiB block `blk` of a stage (columns
+// that are not there: the last eight that are; `valid` is a multiple of 8)
+template <int DIM>
+static __device__ __forceinline__ uint32_t strided_lane_offset(int blk, int lane, int valid, int64_t ld)
+{
+    constexpr int SLOTS = DIM / 8;
+    const int at = blk * 64 + lane, row = at / SLOTS, slot = (at % SLOTS) ^ strided_swizzle<DIM>(row);
+    return (uint32_t)(((int64_t)row * ld + min(slot, valid / 8 - 1) * 8) * 2);
+}
+// A of a KStrided operand: see PlainA
+template <class T>
+struct StridedA {
+    uint32_t off[T::AB];
+    const uint16_t *base;
+    int64_t step;
+    __device__ __forceinline__ StridedA(const uint16_t *a_tile, int rows_valid, int64_t lda, int wave, int lane) : base(scalar_base(a_tile)), step(lda * T::BK)
+    {
+#pragma unroll
+        for (int i = 0; i < T::AB; ++i) off[i] = strided_lane_offset<T::BM>(wave * T::AB + i, lane, rows_valid, lda);
+    }
+    __device__ __forceinline__ void seek(int) {}
+    __device__ __forceinline__ const uint16_t *at(int kt) const { return base + kt * step; }
+};
+typedef short i16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4_t lds_i16x4_t;
+// A fragment (16 rows of the operand, 32 k values) out of a KStrided stage: addr = LDS address of the lane's part
+template <int DIM>
+static __device__ __forceinline__ bf16x8_t strided_fragment(uint32_t addr)
+{
+    union { i16x4_t h[2]; bf16x8_t v; } n;
+    n.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(uintptr_t)addr);
+    n.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4_t *)(uintptr_t)(addr + 4 * DIM * 2));
+    return n.v;
+}
+
 // One MFMA: 16 columns of the packed weight x 16 rows of A x 32 k. The operands are passed swapped (D[n][m]), so that
 // a lane ends up with 4 consecutive columns of one C row. Inline assembly with the accumulator tied to the
 // accumulation registers: the builtin leaves the register allocator free to move the 256 of the big tile between the
@@ -297,12 +346,13 @@ static __device__ __forceinline__ void tile_accumulate_burst(TileAcc<T> &ta, Add
 // MFMAs behind it); M0 written a slot ahead of its load 1552; this loop's row-segment stores 1556. The loop before it
 // (32x32x16, one barrier per turn, the loads of a k-tile within half a turn) 1244; the vendor library 1596-1650.
 // Counters (M 16384, K 8192, N 3584): 2446 cycles a turn, epilogues included, of which 2048 are MFMAs.
-template <class T, class Hook = NoHook, class AddrA = PlainA<T>>
+template <class T, class Hook = NoHook, class AddrA = PlainA<T>, class LayA = KContiguous, class LayB = KContiguous>
 static __device__ __forceinline__ void tile_accumulate_from(TileAcc<T> &ta, AddrA &pa,
                                                             const uint16_t *__restrict__ wt_tile, int cols_valid,
                                                             int64_t ldw, int K, unsigned char *smem,
                                                             Hook after_first_wait = Hook())
 {
+    static_assert(!T::BURST || (!LayA::STRIDED && !LayB::STRIDED), "the paired loop reads k-contiguous operands");
     if constexpr (T::BURST) {
         tile_accumulate_burst<T, Hook, AddrA>(ta, pa, wt_tile, cols_valid, ldw, K, smem, after_first_wait);
         return;
@@ -318,7 +368,10 @@ static __device__ __forceinline__ void tile_accumulate_from(TileAcc<T> &ta, Addr
 
     uint32_t offb[T::BB];                  // per-lane byte offsets of the W loads from the tile's first row
 #pragma unroll
-    for (int i = 0; i < T::BB; ++i) offb[i] = lane_offset<T>(wave * T::BB + i, lane, cols_valid, ldw);
+    for (int i = 0; i < T::BB; ++i) {
+        if constexpr (LayB::STRIDED) offb[i] = strided_lane_offset<T::BN>(wave * T::BB + i, lane, cols_valid, ldw);
+        else offb[i] = lane_offset<T>(wave * T::BB + i, lane, cols_valid, ldw);
+    }
     // load l of the wavefront's LOADS loads of a k-tile: first the AB blocks of A, then the BB blocks of W (k-tiles are
     // issued in ascending order; load 0 of a k-tile comes first)
     const uint32_t lds_a = lds0 + wave * T::AB * 1024, lds_b = lds0 + T::A_STAGE + wave * T::BB * 1024;
@@ -331,6 +384,7 @@ static __device__ __forceinline__ void tile_accumulate_from(TileAcc<T> &ta, Addr
         constexpr int l = decltype(l_c)::value;
         if constexpr (l == 0) pa.seek(kt);
         if constexpr (l < T::AB) load_to_lds_16(pa.at(kt), pa.off[l]);
+        else if constexpr (LayB::STRIDED) load_to_lds_16(wt + kt * (ldw * T::BK), offb[l - T::AB]);
         else load_to_lds_16(wt + (int64_t)kt * T::BK, offb[l - T::AB]);
     };
 
@@ -339,16 +393,46 @@ static __device__ __forceinline__ void tile_accumulate_from(TileAcc<T> &ta, Addr
     const int frow = lane & 15, fh = lane >> 4, fs = (frow >> 1) & 7;
     const int a_base = (wm * T::WTM + frow) * T::ROWB;
     const int b_base = T::A_STAGE + (wn * T::WTN + frow) * T::ROWB;
+    // ... of KStrided operands: the lane's row among 32 and its place in the row, and the swizzle of it in bytes
+    const int trow = 8 * fh + (frow >> 2);
+    const uint32_t t_low = ((frow & 3) >> 1) * 16 + (frow & 1) * 8;
+    uint32_t ta_lane = 0, ta_swz = 0, tb_lane = 0, tb_swz = 0;
+    if constexpr (LayA::STRIDED) {
+        ta_lane = lds0 + trow * T::BM * 2 + t_low;
+        ta_swz = strided_swizzle<T::BM>(trow) * 16;
+    }
+    if constexpr (LayB::STRIDED) {
+        tb_lane = lds0 + T::A_STAGE + trow * T::BN * 2 + t_low;
+        tb_swz = strided_swizzle<T::BN>(trow) * 16;
+    }
     bf16x8_t fa[2][T::FM], fb[2][T::FN];
+    auto read_a = [&](uint32_t stage, auto half_c, auto i_c) __attribute__((always_inline)) {
+        constexpr int half = decltype(half_c)::value, i = decltype(i_c)::value;
+        if constexpr (LayA::STRIDED) {
+            fa[half][i] = strided_fragment<T::BM>(stage + half * 32 * T::BM * 2 + ta_lane + (((wm * T::WTM + i * 16) * 2) ^ ta_swz));
+        } else {
+            const int slot = ((4 * half + fh) ^ fs) << 4;
+            const unsigned char *base = smem + stage + slot;
+            fa[half][i] = *reinterpret_cast<const bf16x8_t *>(base + a_base + i * 16 * T::ROWB);
+        }
+    };
+    auto read_b = [&](uint32_t stage, auto half_c, auto j_c) __attribute__((always_inline)) {
+        constexpr int half = decltype(half_c)::value, j = decltype(j_c)::value;
+        if constexpr (LayB::STRIDED) {
+            fb[half][j] = strided_fragment<T::BN>(stage + half * 32 * T::BN * 2 + tb_lane + (((wn * T::WTN + j * 16) * 2) ^ tb_swz));
+        } else {
+            const int slot = ((4 * half + fh) ^ fs) << 4;
+            const unsigned char *base = smem + stage + slot;
+            fb[half][j] = *reinterpret_cast<const bf16x8_t *>(base + b_base + j * 16 * T::ROWB);
+        }
+    };
     // fragment q of the FM + FN fragments of a half: the order of their first use (row block 0, every column block,
     // the other row blocks)
     auto read_frag = [&](uint32_t stage, auto half_c, auto q_c) __attribute__((always_inline)) {
-        constexpr int half = decltype(half_c)::value, q = decltype(q_c)::value;
-        const int slot = ((4 * half + fh) ^ fs) << 4;
-        const unsigned char *base = smem + stage + slot;
-        if constexpr (q == 0) fa[half][0] = *reinterpret_cast<const bf16x8_t *>(base + a_base);
-        else if constexpr (q <= T::FN) fb[half][q - 1] = *reinterpret_cast<const bf16x8_t *>(base + b_base + (q - 1) * 16 * T::ROWB);
-        else fa[half][q - T::FN] = *reinterpret_cast<const bf16x8_t *>(base + a_base + (q - T::FN) * 16 * T::ROWB);
+        constexpr int q = decltype(q_c)::value;
+        if constexpr (q == 0) read_a(stage, half_c, std::integral_constant<int, 0>{});
+        else if constexpr (q <= T::FN) read_b(stage, half_c, std::integral_constant<int, q - 1>{});
+        else read_a(stage, half_c, std::integral_constant<int, q - T::FN>{});
     };
     constexpr std::integral_constant<int, 0> first{};
     constexpr std::integral_constant<int, 1> second{};

@@ -81,7 +81,7 @@ def within(got, ref, tol, what):
 
 # one row to more than a tile of each kind, odd ones; k of one k-tile to many; columns that fill no tile and no lane's eight
 SIZES = [(1, 64, 8), (1, 4096, 768), (3, 128, 40), (16, 2112, 264), (17, 64, 520), (33, 512, 72), (64, 4096, 768), (65, 1024, 200), (127, 192, 1032), (300, 576, 1160), (1000, 320, 328),
-         (2311, 128, 2056), (4100, 64, 1544), (530, 8192, 136)]
+         (2311, 128, 2056), (4100, 64, 1544), (530, 8192, 136), (198, 13440, 2392), (1404, 13888, 464)]
 
 
 @pytest.mark.parametrize("kn", [True, False], ids=["kn", "nk"])
@@ -293,7 +293,44 @@ def test_refusals_on_the_device(gpu):
         refused(F.ficco_linear, *args)
         args[k] = host.pin_memory()
         refused(F.ficco_linear, *args)
-    big = F.ficco_linear_t(M=4096, K=4096, N=4096)
-    refused(F.ficco_linear, big, t, t, None, None, None, t, None, 0, gpu["cs"])
-    refused(F.ficco_linear, big, t, t, None, None, None, t, t, 2 * 4096 * 4096 - 1, gpu["cs"])
+    # (buffers as large as the call says, should it be taken)
+    big = F.ficco_linear_t(M=198, K=13440, N=2392)
+    n = F.ficco_linear_workspace(big)
+    assert n == 2 * 13440 * 2392
+    A, W, C, ws = [torch.zeros(k, dtype=torch.bfloat16, device=gpu["dev"]) for k in (198 * 13440, 13440 * 2392, 198 * 2392, 13440 * 2392)]
+    refused(F.ficco_linear, big, A, W, None, None, None, C, None, 0, gpu["cs"])
+    refused(F.ficco_linear, big, A, W, None, None, None, C, ws, n - 1, gpu["cs"])
     refused(F.ficco_linear_backward, op, t, t, None, t, t, t, None, t, F.ficco_linear_workspace(op, True) - 1, gpu["cs"])
+
+
+@pytest.mark.parametrize("kn", [True, False], ids=["kn", "nk"])
+@pytest.mark.parametrize("M,K,N", [(256, 256, 512), (512, 2048, 1024), (1024, 1152, 1544), (2048, 832, 2112), (4096, 512, 384), (8192, 64, 72), (128, 4096, 4096)])
+def test_products_that_read_their_operands_as_they_are(gpu, M, K, N, kn):
+    """Row counts that are whole k-tiles, at which dW reads A and dZ in place, and [K,N] weights large enough for the tiles that read
+    them in place: forward, and backward with and without an activation."""
+    normal = seeded(gpu, M + K * 3 + N)
+    A, W, dC, z, bias = normal(M, K), weight(normal, K, N, kn), normal(M, N), normal(M, N, std=1.5), normal(N)
+    Wk = (W if kn else W.t()).double()
+    for kind in ("none", "gelu_tanh"):
+        op = F.ficco_linear_t(M=M, K=K, N=N, weight_layout=int(not kn), activation=ACTS[kind])
+        C = torch.full((M + 1, N), 99.0, dtype=torch.bfloat16, device=gpu["dev"])
+        print("ficco_linear", M, K, N, "kn" if kn else "nk", kind, flush=True)
+        forward(gpu, op, A, W, bias, None, None, C)
+        v = A.double() @ Wk + bias.double()
+        ref = act64(v, kind)
+        within(C[:M], ref, (U + 2 * E) * ref.abs() + 2.26 * (K + 2) * E * (A.double().abs() @ Wk.abs() + bias.double().abs()) + 4e-6 * v.abs(), f"C {kind}")
+        assert (C[M] == 99).all()
+        dA = torch.full((M + 1, K), 99.0, dtype=torch.bfloat16, device=gpu["dev"])
+        dW = torch.full((W.shape[0] + 1, W.shape[1]), 99.0, dtype=torch.bfloat16, device=gpu["dev"])
+        db = torch.empty(N, device=gpu["dev"])
+        backward(gpu, op, A, W, None if kind == "none" else z, dC, dA, dW, db)
+        dz = dC.double() if kind == "none" else dC.double() * slope64(z.double(), kind)
+        rounded = 0 if kind == "none" else U
+        wref, wsize = A.double().t() @ dz, A.double().t().abs() @ dz.abs()
+        if not kn:
+            wref, wsize = wref.t(), wsize.t()
+        for name, got, ref, size, terms in [("dA", dA[:M], dz @ Wk.t(), dz.abs() @ Wk.t().abs(), N), ("dW", dW[:-1], wref, wsize, M)]:
+            within(got, ref, U * ref.abs() + (rounded * 1.01 + 2 * (terms + 64) * E + 4e-6) * size, f"{name} {kind}")
+            assert (got.double() - ref).norm() <= 3.4e-3 * ref.norm(), (name, kind)
+        within(db, dz.sum(0), (M + 2) * E * dz.abs().sum(0) + 4e-6 * dC.double().abs().sum(0), f"dbias {kind}")
+        assert (dA[M] == 99).all() and (dW[-1] == 99).all()

@@ -60,14 +60,17 @@ def test_linear_pointers():
 
 def test_linear_workspace_holds_what_is_laid_out():
     t = F.ficco_linear_t
-    # a large [K,N] weight is re-laid out, an [N,K] one and that of a few rows are not
-    assert F.ficco_linear_workspace(t(M=4096, K=4096, N=4096)) == 2 * 4096 * 4096
-    assert F.ficco_linear_workspace(t(M=4096, K=4096, N=4096, weight_layout=F.FICCO_WEIGHT_NK)) == 0
-    assert F.ficco_linear_workspace(t(M=16, K=1024, N=512)) == 0
+    # a [K,N] weight is re-laid out where parts of tiles are the fastest, and read in place elsewhere, as an [N,K] one is
+    assert F.ficco_linear_workspace(t(M=198, K=13440, N=2392)) == 2 * 13440 * 2392
+    assert F.ficco_linear_workspace(t(M=198, K=13440, N=2392, weight_layout=F.FICCO_WEIGHT_NK)) == 0
+    assert F.ficco_linear_workspace(t(M=4096, K=4096, N=4096)) == 0 == F.ficco_linear_workspace(t(M=16, K=1024, N=512))
     assert F.ficco_linear_workspace(t(M=0, K=4096, N=4096)) == 0 == F.ficco_linear_workspace(t(M=0, K=4096, N=4096), True)
-    # dZ in both orders, A turned and the column sums; M and N to whole k-tiles
+    # dZ in both orders, A turned and the column sums; M and N to whole k-tiles. With whole k-tiles of rows A stays as it is
     least = 2 * (100 * 128 + 72 * 128 + 64 * 128 + 64 * 128)
     assert least <= F.ficco_linear_workspace(t(M=100, K=64, N=72, activation=F.FICCO_ACT_SILU), True) <= least + 8192
+    z = 2 * 8192 * 4096
+    assert 2 * z <= F.ficco_linear_workspace(t(M=8192, K=8192, N=4096, activation=F.FICCO_ACT_SILU), True) <= 2 * z + 128 * 4096 * 4 + 8192
+    assert z <= F.ficco_linear_workspace(t(M=8192, K=8192, N=4096), True) <= z + 128 * 4096 * 4 + 8192
 
 
 def norm(backward=False, **k):
