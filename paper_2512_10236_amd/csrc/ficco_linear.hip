@@ -42,14 +42,16 @@ int tile_for(int64_t M, int64_t K, int64_t N, double *us)
 // of them, and read as fragments. The eight partial tiles are added through LDS in the order of the wavefronts. So narrow tiles
 // over all of k, instead of wide ones, spread the weight over as many CUs as there are.
 // Fragments loaded from memory directly, a lane a row: a CU then draws 16 bytes a cycle, one lane's at a time.
-template <int AB_, int NB_>
+template <int AB_, int NB_, bool SB_>
 struct RowsCfg {
+    static constexpr bool SB = SB_;                            // the weight is [K,N]
     static constexpr int AB = AB_, NB = NB_, WAVES = 8, FM = AB < 2 ? 1 : AB / 2, BM = 8 * AB, BN = 16 * NB;
     static constexpr int LOADS = AB + 2 * NB, STAGE = LOADS * 1024;              // a wavefront's, per k-tile
     static constexpr int D = 160 * 1024 / (WAVES * STAGE) < 6 ? 160 * 1024 / (WAVES * STAGE) : 6;
     static constexpr int RING = D * STAGE, PART = FM * NB * 1024;
     static constexpr int LDS_BYTES = WAVES * (RING > PART ? RING : PART);
     static_assert(D >= 2 && (D - 1) * LOADS < 64, "a ring of two stages or more, vmcnt has 6 bits");
+    static_assert(!SB || NB % 4 == 0, "whole lines of a [K,N] weight's rows");
 };
 constexpr int kRowsThreads = 512;
 
@@ -64,12 +66,18 @@ __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch 
     const int lid = run.start + run.first;
     const int row0 = lid % tiles_m * T::BM, col0 = lid / tiles_m * T::BN;
     const int KT = scalar(a.K) / kBK;
-    const uint16_t *const A = scalar_base(a.A + (int64_t)row0 * a.lda), *const W = scalar_base(a.W + (int64_t)col0 * a.ldw);
+    const uint16_t *const A = scalar_base(a.A + (int64_t)row0 * a.lda), *const W = scalar_base(a.W + (T::SB ? (int64_t)col0 : (int64_t)col0 * a.ldw));
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * T::RING;
     // 16-byte slot c of row r of 16 lies at slot c ^ ((r >> 1) & 7); rows and columns that are not there: the last that is
     uint32_t off[T::LOADS];
 #pragma unroll
     for (int l = 0; l < T::LOADS; ++l) {
+        if constexpr (T::SB) {
+            if (l >= T::AB) {
+                off[l] = strided_lane_offset<T::BN>(l - T::AB, lane, min(T::BN, a.N - col0), a.ldw);
+                continue;
+            }
+        }
         const int r = (l < T::AB ? l : l - T::AB) * 8 + lane / 8;
         const int row = l < T::AB ? min(r, a.M - 1 - row0) : min(r, a.N - 1 - col0);
         off[l] = ((uint32_t)row * (uint32_t)(l < T::AB ? a.lda : a.ldw) + (uint32_t)(((lane % 8) ^ ((r >> 1) & 7)) * 8)) * 2u;
@@ -79,7 +87,7 @@ __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch 
             constexpr int l = decltype(l_c)::value;
             set_lds_target<l * 1024>(ring + stage);
             asm volatile("s_nop 0" ::: "memory");
-            load_to_lds_16((l < T::AB ? A : W) + (int64_t)kt * kBK, off[l]);
+            load_to_lds_16(l < T::AB ? A + (int64_t)kt * kBK : W + (T::SB ? kt * (a.ldw * kBK) : (int64_t)kt * kBK), off[l]);
         });
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -88,6 +96,13 @@ __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch 
     for (int i = 0; i < T::FM; ++i)
 #pragma unroll
         for (int n = 0; n < T::NB; ++n) acc[i][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    // a lane's part of a transposing read (see tile_accumulate_from)
+    const int trow = 8 * g + (j >> 2);
+    uint32_t t_lane = 0, t_swz = 0;
+    if constexpr (T::SB) {
+        t_lane = ring + T::AB * 1024 + trow * T::BN * 2 + ((j & 3) >> 1) * 16 + (j & 1) * 8;
+        t_swz = strided_swizzle<T::BN>(trow) * 16;
+    }
     if (wave < KT) {
         // past the wavefront's last k-tile the loads go on, on that k-tile again and into stages that are not read
         const int last = wave + (KT - 1 - wave) / T::WAVES * T::WAVES;
@@ -106,7 +121,10 @@ __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch 
 #pragma unroll
                 for (int i = 0; i < T::FM; ++i) fa[h][i] = *reinterpret_cast<const bf16x8_t *>(base + (16 * i + (T::AB == 1 ? j & 7 : j)) * 128 + (T::AB == 1 ? ((4 * h + g) ^ (((j & 7) >> 1) & 7)) << 4 : slot));
 #pragma unroll
-                for (int n = 0; n < T::NB; ++n) fw[h][n] = *reinterpret_cast<const bf16x8_t *>(base + T::AB * 1024 + (16 * n + j) * 128 + slot);
+                for (int n = 0; n < T::NB; ++n) {
+                    if constexpr (T::SB) fw[h][n] = strided_fragment<T::BN>(stage + t_lane + h * 32 * T::BN * 2 + ((n * 32) ^ t_swz));
+                    else fw[h][n] = *reinterpret_cast<const bf16x8_t *>(base + T::AB * 1024 + (16 * n + j) * 128 + slot);
+                }
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // the stage has been read: it may be filled again
             __builtin_amdgcn_sched_barrier(0);
@@ -163,11 +181,13 @@ int launch_rows_t(const LinearLaunch &a, hipStream_t s)
     return FICCO_OK;
 }
 
-// Tiles of the few-rows kernel: 8 ab rows x 16 nb columns
-#define FICCO_FOR_EACH_ROWS(X) X(1, 1) X(1, 2) X(1, 4) X(2, 1) X(2, 2) X(2, 4) X(4, 1) X(4, 2) X(8, 1)
-int launch_rows(int ab, int nb, const LinearLaunch &a, hipStream_t s)
+// Tiles of the few-rows kernel: 8 ab rows x 16 nb columns, of an [N,K] weight or of a [K,N] one
+#define FICCO_FOR_EACH_ROWS(X) \
+    X(1, 1, false) X(1, 2, false) X(1, 4, false) X(2, 1, false) X(2, 2, false) X(2, 4, false) X(4, 1, false) X(4, 2, false) X(8, 1, false) \
+    X(1, 4, true)
+int launch_rows(int ab, int nb, bool kn, const LinearLaunch &a, hipStream_t s)
 {
-#define X(AB, NB) if (ab == AB && nb == NB) return launch_rows_t<RowsCfg<AB, NB>>(a, s);
+#define X(AB, NB, SB) if (ab == AB && nb == NB && kn == SB) return launch_rows_t<RowsCfg<AB, NB, SB>>(a, s);
     FICCO_FOR_EACH_ROWS(X)
 #undef X
     return FICCO_ERR_ARG;
@@ -179,23 +199,28 @@ int launch_rows(int ab, int nb, const LinearLaunch &a, hipStream_t s)
 // Fitted to M 1-256 of eight shapes, K 512-16384, N 64-14336, each tile forced in turn (us, the other kernels / the tile taken:
 // M 16, K 8192, N 3584 29.6 / 11.6; M 64 29.9 / 14.9; M 128 29.7 / 25.5; M 256 32.3, its best tile 48.9; M 64, K 4096, N 768 11.8 /
 // 5.5; M 16, K 8192, N 64 18.8 / 5.9; M 64, K 4096, N 14336 21.6, its best tile 32.3).
+// Of a [K,N] weight a workgroup reads 128 bytes of each row, and that is faster than the direct kernel's wider stages only where
+// the weight is small enough to stay in the L2s (us, direct / this one: M 64, K 4096, N 768 9.1 / 7.6; M 2, K 9536, N 312 17.4 /
+// 12.7; M 16, K 9344, N 128 16.9 / 12.3; beyond 8 MiB M 16, K 8192, N 3584 22.9 / 22.2; M 5, K 8704, N 856 22.8 / 23.5; M 7, K 3136,
+// N 4256 8.8 / 9.8) and one round of tiles holds it (M 89, K 1792, N 1464 5.9 / 12.3).
 struct RowsTile {
     int ab, nb;
 };
-RowsTile rows_tile(int64_t M, int64_t K, int64_t N, double us)
+RowsTile rows_tile(int64_t M, int64_t K, int64_t N, bool kn, double us)
 {
     RowsTile best{0, 0};
-    if (M > 256) return best;
+    if (M > 256 || (kn && K * N * 2 > (8 << 20))) return best;
     const int cus = compute_units();
     auto consider = [&](int ab, int nb) {
         if (ab > 1 && M <= 8 * ab / 2) return;                 // half of the rows or more would not be there
         const int64_t tiles = ((M + 8 * ab - 1) / (8 * ab)) * ((N + 16 * nb - 1) / (16 * nb)), full = tiles / cus, rest = tiles - full * cus;
+        if (kn && full) return;
         const double kb = (16 * nb + 8 * ab) * (double)K * 2e-3;
         const double drawn = (double)full * kb / 90 + (rest ? kb / (146.0 - 56.0 * (double)rest / cus) : 0) + 2.5 * (double)((tiles + cus - 1) / cus - 1);
         const double t = 3.0 + std::max(drawn, (double)(N * K + M * K) * 2 / 7.3e6);
         if (t < us * 0.999) { us = t; best = {ab, nb}; }
     };
-#define X(AB, NB) consider(AB, NB);
+#define X(AB, NB, SB) if (kn == SB) consider(AB, NB);
     FICCO_FOR_EACH_ROWS(X)
 #undef X
     return best;
@@ -402,10 +427,12 @@ Forward forward_way(const ficco_linear_t &o)
     double us = 0;
     f.tile = tile_for(o.M, o.K, o.N, &us);
     if (o.weight_layout == FICCO_WEIGHT_KN) {
-        if (o.K * o.N * 2 <= 0x7FFFFFFF) f.row_blocks = direct_row_blocks(o.M, o.K, o.N, compute_units(), us);
-        if (!f.row_blocks && !strided_tile(f.tile, false)) f.bytes = round_up(o.K * o.N * 2, 256);
+        if (o.K * o.N * 2 <= 0x7FFFFFFF) f.row_blocks = direct_row_blocks(o.M, o.K, o.N, compute_units(), us, &us);
+        f.rows = rows_tile(o.M, o.K, o.N, true, us);
+        if (f.rows.ab) f.row_blocks = 0;
+        else if (!f.row_blocks && !strided_tile(f.tile, false)) f.bytes = round_up(o.K * o.N * 2, 256);
     } else {
-        f.rows = rows_tile(o.M, o.K, o.N, us);
+        f.rows = rows_tile(o.M, o.K, o.N, false, us);
     }
     return f;
 }
@@ -512,14 +539,14 @@ int forward(const ficco_linear_t *op, const void *A, const void *W, const void *
         return FICCO_OK;
     }
     LinearLaunch a{(const uint16_t *)A, (const uint16_t *)W, (uint16_t *)C, o.lda, o.K, o.ldc, (int32_t)o.M, (int32_t)o.N, (int32_t)o.K, 0, e};
-    if (f.rows.ab) return launch_rows(f.rows.ab, f.rows.nb, a, s);
-    if (o.weight_layout == FICCO_WEIGHT_KN) {
-        if (!f.bytes) {
-            a.ldw = o.N;
-            return launch_tiles_strided(strided_tile(f.tile, false), false, a, s);
-        }
+    const bool kn = o.weight_layout == FICCO_WEIGHT_KN;
+    if (kn) a.ldw = o.N;
+    if (f.rows.ab) return launch_rows(f.rows.ab, f.rows.nb, kn, a, s);
+    if (kn) {
+        if (!f.bytes) return launch_tiles_strided(strided_tile(f.tile, false), false, a, s);
         HIP_TRY(launch_pack_weight((const uint16_t *)W, (uint16_t *)workspace, o.K, o.N, s));
         a.W = (const uint16_t *)workspace;
+        a.ldw = o.K;
     }
     return launch_tiles(f.tile, a, s);
 }

@@ -198,6 +198,8 @@ int choose_tile(const ficco_plan_t *p, int cus, bool whole_rows = false, double 
 inline int64_t widest_lists(int64_t N) { return (N + 127) / 128; }
 // ficco_gemm_static: row blocks (1, 2 or 4) of the direct kernel, 0 = pack the weight first, which takes packed_us
 int direct_row_blocks(int64_t M, int64_t K, int64_t N, int cus, double packed_us);
+// ... and the estimate, if it is not 0
+int direct_row_blocks(int64_t M, int64_t K, int64_t N, int cus, double packed_us, double *us);
 inline bool overlap(const void *a, int64_t a_bytes, const void *b, int64_t b_bytes)
 {
     return (uintptr_t)a < (uintptr_t)b + (uintptr_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uintptr_t)a_bytes;

@@ -46,7 +46,7 @@ int scratch_of(int dev, unsigned char **out)
 // taken is 0.1 % slower than the fastest (0.4 with 0.55, 1.5 and 4 in the place of 0.46, 2 and 6; calls under 4.6 us, which
 // the host takes, count as that). Measured, direct against packed: M 576, K 4224, N 992 16.3 : 22.7, M 1225, K 2496, N 904
 // 22.0 : 20.9, M 1596, K 1600, N 1880 27.3 : 21.5, M 2594, K 4096, N 680 39.6 : 27.4.
-int direct_row_blocks(int64_t M, int64_t K, int64_t N, int cus, double packed_us)
+int direct_row_blocks(int64_t M, int64_t K, int64_t N, int cus, double packed_us, double *us)
 {
     static const struct { int row_blocks; double stage; } cand[] = {{1, 0.25}, {2, 0.31}, {4, 0.46}};
     double best = packed_us + 6.0;
@@ -56,8 +56,10 @@ int direct_row_blocks(int64_t M, int64_t K, int64_t N, int cus, double packed_us
         const double t = (double)((tiles + cus - 1) / cus) * (2.0 + cd.stage * (double)((K + 127) / 128)) + 2.0;
         if (t < best) { best = t; best_id = cd.row_blocks; }
     }
+    if (us && best_id) *us = best;
     return best_id;
 }
+int direct_row_blocks(int64_t M, int64_t K, int64_t N, int cus, double packed_us) { return direct_row_blocks(M, K, N, cus, packed_us, nullptr); }
 
 }  // namespace ficco
 
