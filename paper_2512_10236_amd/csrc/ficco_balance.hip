@@ -328,7 +328,7 @@ int lanes_of(int experts) { return experts <= 8 ? 8 : experts <= 16 ? 16 : exper
 struct Chunks {
     int64_t groups, per_group, tokens;
 };
-// Chunks for about four workgroups a CU of 256 CUs; a group whose tokens a workgroup takes in 16 turns or fewer is one chunk,
+// Chunks for about four workgroups a CU of 256 CUs; a group whose tokens a workgroup takes in 32 turns or fewer is one chunk,
 // which spares the launches that join them.
 Chunks chunks_of(const ficco_expert_balance_t &o)
 {
@@ -336,7 +336,7 @@ Chunks chunks_of(const ficco_expert_balance_t &o)
     c.groups = (o.tokens + o.group_tokens - 1) / o.group_tokens;
     const int64_t turn = 256 / lanes_of(o.experts);
     const int64_t each = std::max((o.tokens + 1023) / 1024, turn);
-    c.per_group = o.group_tokens <= 16 * turn ? 1 : (o.group_tokens + each - 1) / each;
+    c.per_group = o.group_tokens <= 32 * turn ? 1 : (o.group_tokens + each - 1) / each;
     c.tokens = (o.group_tokens + c.per_group - 1) / c.per_group;
     return c;
 }

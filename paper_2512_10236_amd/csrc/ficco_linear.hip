@@ -55,17 +55,19 @@ struct RowsCfg {
 };
 constexpr int kRowsThreads = 512;
 
+// splits > 1: the workgroups of a tile share k, each a run of k-tiles, and write fp32 sums to part [splits][M][N], which
+// linear_join_kernel adds in order. For a long k over few columns, where the tiles leave most CUs idle.
 template <class T>
-__global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch a)
+__global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch a, int splits, float *part)
 {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const int lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), j = lane & 15, g = lane >> 4;
     // tiles in 8 runs, one per XCD, rows fastest: the row tiles that read the same columns of the weight share an L2
     const int tiles_m = (a.M + T::BM - 1) / T::BM, tiles_n = (a.N + T::BN - 1) / T::BN;
-    const XcdRun run = xcd_run(blockIdx.x, gridDim.x, tiles_m * tiles_n);
-    const int lid = run.start + run.first;
-    const int row0 = lid % tiles_m * T::BM, col0 = lid / tiles_m * T::BN;
-    const int KT = scalar(a.K) / kBK;
+    const XcdRun run = xcd_run(blockIdx.x, gridDim.x, tiles_m * tiles_n * splits);
+    const int lid = run.start + run.first, rest = lid / tiles_m, split = rest % splits;
+    const int row0 = lid % tiles_m * T::BM, col0 = rest / splits * T::BN;
+    const int k_tiles = scalar(a.K) / kBK, KT = scalar((int)((int64_t)(split + 1) * k_tiles / splits)), kt0 = scalar((int)((int64_t)split * k_tiles / splits)) + wave;
     const uint16_t *const A = scalar_base(a.A + (int64_t)row0 * a.lda), *const W = scalar_base(a.W + (T::SB ? (int64_t)col0 : (int64_t)col0 * a.ldw));
     const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem + wave * T::RING;
     // 16-byte slot c of row r of 16 lies at slot c ^ ((r >> 1) & 7); rows and columns that are not there: the last that is
@@ -103,14 +105,14 @@ __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch 
         t_lane = ring + T::AB * 1024 + trow * T::BN * 2 + ((j & 3) >> 1) * 16 + (j & 1) * 8;
         t_swz = strided_swizzle<T::BN>(trow) * 16;
     }
-    if (wave < KT) {
+    if (kt0 < KT) {
         // past the wavefront's last k-tile the loads go on, on that k-tile again and into stages that are not read
-        const int last = wave + (KT - 1 - wave) / T::WAVES * T::WAVES;
+        const int last = kt0 + (KT - 1 - kt0) / T::WAVES * T::WAVES;
 #pragma unroll
-        for (int d = 0; d < T::D; ++d) issue(min(wave + d * T::WAVES, last), d * T::STAGE);
+        for (int d = 0; d < T::D; ++d) issue(min(kt0 + d * T::WAVES, last), d * T::STAGE);
         uint32_t stage = 0;
 #pragma clang loop unroll(disable)
-        for (int kt = wave; kt < KT; kt += T::WAVES) {
+        for (int kt = kt0; kt < KT; kt += T::WAVES) {
             wait_vmem<(T::D - 1) * T::LOADS>();
             __builtin_amdgcn_sched_barrier(0);
             const unsigned char *const base = smem + wave * T::RING + stage;
@@ -140,17 +142,17 @@ __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch 
         wait_vmem<0>();                    // no load may arrive in LDS that is used for something else
     }
     __syncthreads();
-    f32x4_t *const part = reinterpret_cast<f32x4_t *>(smem);
+    f32x4_t *const tile = reinterpret_cast<f32x4_t *>(smem);
 #pragma unroll
     for (int i = 0; i < T::FM; ++i)
 #pragma unroll
-        for (int n = 0; n < T::NB; ++n) part[(wave * T::FM * T::NB + i * T::NB + n) * 64 + lane] = acc[i][n];
+        for (int n = 0; n < T::NB; ++n) tile[(wave * T::FM * T::NB + i * T::NB + n) * 64 + lane] = acc[i][n];
     __syncthreads();
     for (int q = wave; q < T::FM * T::NB; q += T::WAVES) {
-        f32x4_t z = part[q * 64 + lane];
+        f32x4_t z = tile[q * 64 + lane];
 #pragma unroll
         for (int w = 1; w < T::WAVES; ++w) {
-            const f32x4_t t = part[(w * T::FM * T::NB + q) * 64 + lane];
+            const f32x4_t t = tile[(w * T::FM * T::NB + q) * 64 + lane];
 #pragma unroll
             for (int v = 0; v < 4; ++v) z[v] += t[v];
         }
@@ -158,17 +160,38 @@ __global__ __launch_bounds__(kRowsThreads) void linear_rows_kernel(LinearLaunch 
         const int64_t m = row0 + 16 * (q / T::NB) + j;
         const int n = col0 + 16 * (q % T::NB) + 4 * g;
         if (m < min(a.M, row0 + T::BM) && n < a.N) {
+            if (splits > 1) {
+                *reinterpret_cast<f32x4_t *>(part + ((int64_t)split * a.M + m) * a.N + n) = z;
+                continue;
+            }
             const f32x4_t bias = bias4(a.e, n);
             with_activation(a.e.activation, [&](auto act) __attribute__((always_inline)) { store4<act.value>(a.e, z, bias, a.C + m * a.ldc + n, m, n); });
         }
     }
 }
 
-template <class T>
-int launch_rows_t(const LinearLaunch &a, hipStream_t s)
+__global__ __launch_bounds__(256) void linear_join_kernel(LinearLaunch a, int splits, const float *__restrict__ part)
 {
-    const int64_t tiles = (((int64_t)a.M + T::BM - 1) / T::BM) * (((int64_t)a.N + T::BN - 1) / T::BN);
-    if (tiles > 0x7FFFFFFF / kRowsThreads) return FICCO_ERR_SHAPE;
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4, plane = (int64_t)a.M * a.N;
+    if (at >= plane) return;
+    f32x4_t z = *reinterpret_cast<const f32x4_t *>(part + at);
+#pragma unroll 4
+    for (int k = 1; k < splits; ++k) {
+        const f32x4_t t = *reinterpret_cast<const f32x4_t *>(part + k * plane + at);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) z[v] += t[v];
+    }
+    const int64_t m = at / a.N;
+    const int n = (int)(at - m * a.N);
+    const f32x4_t bias = bias4(a.e, n);
+    with_activation(a.e.activation, [&](auto act) __attribute__((always_inline)) { store4<act.value>(a.e, z, bias, a.C + m * a.ldc + n, m, n); });
+}
+
+template <class T>
+int launch_rows_t(const LinearLaunch &a, int splits, float *part, hipStream_t s)
+{
+    const int64_t tiles = (((int64_t)a.M + T::BM - 1) / T::BM) * (((int64_t)a.N + T::BN - 1) / T::BN) * splits;
+    if (splits < 1 || (splits > 1 && !part) || tiles > 0x7FFFFFFF / kRowsThreads) return FICCO_ERR_SHAPE;
     static bool set[64];                   // per device
     int dev = 0;
     HIP_TRY(hipGetDevice(&dev));
@@ -176,18 +199,22 @@ int launch_rows_t(const LinearLaunch &a, hipStream_t s)
         HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(&linear_rows_kernel<T>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES));
         if (dev < 64) set[dev] = true;
     }
-    hipLaunchKernelGGL(linear_rows_kernel<T>, dim3((unsigned)tiles), dim3(kRowsThreads), T::LDS_BYTES, s, a);
+    hipLaunchKernelGGL(linear_rows_kernel<T>, dim3((unsigned)tiles), dim3(kRowsThreads), T::LDS_BYTES, s, a, splits, part);
     HIP_TRY(hipGetLastError());
+    if (splits > 1) {
+        hipLaunchKernelGGL(linear_join_kernel, dim3((unsigned)(((int64_t)a.M * a.N / 4 + 255) / 256)), dim3(256), 0, s, a, splits, part);
+        HIP_TRY(hipGetLastError());
+    }
     return FICCO_OK;
 }
 
 // Tiles of the few-rows kernel: 8 ab rows x 16 nb columns, of an [N,K] weight or of a [K,N] one
 #define FICCO_FOR_EACH_ROWS(X) \
     X(1, 1, false) X(1, 2, false) X(1, 4, false) X(2, 1, false) X(2, 2, false) X(2, 4, false) X(4, 1, false) X(4, 2, false) X(8, 1, false) \
-    X(1, 4, true)
-int launch_rows(int ab, int nb, bool kn, const LinearLaunch &a, hipStream_t s)
+    X(1, 4, true) X(2, 4, true)
+int launch_rows(int ab, int nb, bool kn, const LinearLaunch &a, int splits, float *part, hipStream_t s)
 {
-#define X(AB, NB, SB) if (ab == AB && nb == NB && kn == SB) return launch_rows_t<RowsCfg<AB, NB, SB>>(a, s);
+#define X(AB, NB, SB) if (ab == AB && nb == NB && kn == SB) return launch_rows_t<RowsCfg<AB, NB, SB>>(a, splits, part, s);
     FICCO_FOR_EACH_ROWS(X)
 #undef X
     return FICCO_ERR_ARG;
@@ -199,30 +226,57 @@ int launch_rows(int ab, int nb, bool kn, const LinearLaunch &a, hipStream_t s)
 // Fitted to M 1-256 of eight shapes, K 512-16384, N 64-14336, each tile forced in turn (us, the other kernels / the tile taken:
 // M 16, K 8192, N 3584 29.6 / 11.6; M 64 29.9 / 14.9; M 128 29.7 / 25.5; M 256 32.3, its best tile 48.9; M 64, K 4096, N 768 11.8 /
 // 5.5; M 16, K 8192, N 64 18.8 / 5.9; M 64, K 4096, N 14336 21.6, its best tile 32.3).
-// Of a [K,N] weight a workgroup reads 128 bytes of each row, and that is faster than the direct kernel's wider stages only where
-// the weight is small enough to stay in the L2s (us, direct / this one: M 64, K 4096, N 768 9.1 / 7.6; M 2, K 9536, N 312 17.4 /
-// 12.7; M 16, K 9344, N 128 16.9 / 12.3; beyond 8 MiB M 16, K 8192, N 3584 22.9 / 22.2; M 5, K 8704, N 856 22.8 / 23.5; M 7, K 3136,
-// N 4256 8.8 / 9.8) and one round of tiles holds it (M 89, K 1792, N 1464 5.9 / 12.3).
 struct RowsTile {
-    int ab, nb;
+    int ab, nb, splits;
 };
-RowsTile rows_tile(int64_t M, int64_t K, int64_t N, bool kn, double us)
+RowsTile rows_tile(int64_t M, int64_t K, int64_t N, double us)
 {
-    RowsTile best{0, 0};
-    if (M > 256 || (kn && K * N * 2 > (8 << 20))) return best;
+    RowsTile best{0, 0, 1};
+    if (M > 512) return best;
     const int cus = compute_units();
     auto consider = [&](int ab, int nb) {
         if (ab > 1 && M <= 8 * ab / 2) return;                 // half of the rows or more would not be there
         const int64_t tiles = ((M + 8 * ab - 1) / (8 * ab)) * ((N + 16 * nb - 1) / (16 * nb)), full = tiles / cus, rest = tiles - full * cus;
-        if (kn && full) return;
         const double kb = (16 * nb + 8 * ab) * (double)K * 2e-3;
         const double drawn = (double)full * kb / 90 + (rest ? kb / (146.0 - 56.0 * (double)rest / cus) : 0) + 2.5 * (double)((tiles + cus - 1) / cus - 1);
         const double t = 3.0 + std::max(drawn, (double)(N * K + M * K) * 2 / 7.3e6);
-        if (t < us * 0.999) { us = t; best = {ab, nb}; }
+        if (t < us * 0.999) { us = t; best = {ab, nb, 1}; }
     };
-#define X(AB, NB, SB) if (kn == SB) consider(AB, NB);
+#define X(AB, NB, SB) if (!SB) consider(AB, NB);
     FICCO_FOR_EACH_ROWS(X)
 #undef X
+    return best;
+}
+
+// The same of a [K,N] weight, against the direct kernel (row_blocks, us: what that would take) or, row_blocks = 0, a tile's us. A workgroup
+// reads 128 bytes of each row of the weight, and k may be split over as many workgroups as make one round, joined by a second launch.
+// Which is the fastest depends on where the weight comes from: a CU draws 146-90 KB a us of it from the L2s and about 42 from memory,
+// whatever the kernel. A loop over one layer finds a weight of up to 16 MiB in the L2s, a model's layers in turn do not; up to there the
+// rule goes by the geometric mean of both. us, direct / one launch / splits (one layer | layers in turn): M 64, K 4096, N 768 9.1 / 7.6 /
+// 9.5 | 15.3 / 14.4 / 11.6; M 1, K 11456, N 72 20.1 / 14.7 / - | -; M 3, K 4800, N 560 - | 20.9 / 22.9 / 11.7; beyond M 16, K 8192, N 3584
+// - | 38 / 36 / 20; M 1, K 8192, N 1280 29 / 31 / 13; M 166, K 13184, N 264 50 / 43 / 19; M 32, K 16384, N 4096 68 / 61 / 42.
+RowsTile rows_tile_kn(int64_t M, int64_t K, int64_t N, int row_blocks, double us)
+{
+    RowsTile best{0, 0, 1};
+    if (M > 512) return best;
+    const int cus = compute_units();
+    const bool warm = K * N * 2 <= (16 << 20);
+    auto both = [&](double in_l2, double from_memory) { return warm ? sqrt(in_l2 * std::max(in_l2, from_memory)) : from_memory; };
+    if (row_blocks) {
+        const int64_t tiles = ((M + 16 * row_blocks - 1) / (16 * row_blocks)) * ((N + 63) / 64);
+        us = both(std::max(3.5, us - 2.5), 3.0 + (double)((tiles + cus - 1) / cus) * (16 * row_blocks + 64) * (double)K * 2e-3 / 43);
+    }
+    for (int ab = 1; ab <= 2; ++ab) {
+        if (ab > 1 && M <= 8) break;
+        const int64_t tiles = ((M + 8 * ab - 1) / (8 * ab)) * ((N + 63) / 64);
+        for (int splits = 1; splits <= 16 && tiles * splits <= cus; splits *= 2) {
+            if (splits > 1 && K / kBK < splits * 8) break;             // a k-tile for each wavefront
+            const double kb = (64 + 8 * ab) * (double)K * 2e-3 / splits, drawn = kb / (146.0 - 56.0 * (double)(tiles * splits) / cus);
+            const double bytes = (double)(N * K + M * K) * 2 + (splits > 1 ? (double)splits * (double)(M * N) * 8 : 0);
+            const double t = splits > 1 ? both(8.5 + drawn, 8.5 + std::max(kb / 43, bytes / 4.9e6)) : both(3.0 + drawn, 5.0 + std::max(kb / 42, bytes / 4.9e6));
+            if (t < us * (splits > 1 && best.splits == 1 ? 0.9 : 0.97)) { us = t; best = {ab, 4, splits}; }
+        }
+    }
     return best;
 }
 
@@ -428,12 +482,13 @@ Forward forward_way(const ficco_linear_t &o)
     f.tile = tile_for(o.M, o.K, o.N, &us);
     if (o.weight_layout == FICCO_WEIGHT_KN) {
         if (o.K * o.N * 2 <= 0x7FFFFFFF) f.row_blocks = direct_row_blocks(o.M, o.K, o.N, compute_units(), us, &us);
-        f.rows = rows_tile(o.M, o.K, o.N, true, us);
+        f.rows = rows_tile_kn(o.M, o.K, o.N, f.row_blocks, us);
         if (f.rows.ab) f.row_blocks = 0;
         else if (!f.row_blocks && !strided_tile(f.tile, false)) f.bytes = round_up(o.K * o.N * 2, 256);
     } else {
-        f.rows = rows_tile(o.M, o.K, o.N, false, us);
+        f.rows = rows_tile(o.M, o.K, o.N, us);
     }
+    if (f.rows.ab && f.rows.splits > 1) f.bytes = round_up(f.rows.splits * o.M * o.N * 4, 256);
     return f;
 }
 
@@ -541,7 +596,7 @@ int forward(const ficco_linear_t *op, const void *A, const void *W, const void *
     LinearLaunch a{(const uint16_t *)A, (const uint16_t *)W, (uint16_t *)C, o.lda, o.K, o.ldc, (int32_t)o.M, (int32_t)o.N, (int32_t)o.K, 0, e};
     const bool kn = o.weight_layout == FICCO_WEIGHT_KN;
     if (kn) a.ldw = o.N;
-    if (f.rows.ab) return launch_rows(f.rows.ab, f.rows.nb, kn, a, s);
+    if (f.rows.ab) return launch_rows(f.rows.ab, f.rows.nb, kn, a, f.rows.splits, (float *)workspace, s);
     if (kn) {
         if (!f.bytes) return launch_tiles_strided(strided_tile(f.tile, false), false, a, s);
         HIP_TRY(launch_pack_weight((const uint16_t *)W, (uint16_t *)workspace, o.K, o.N, s));
@@ -580,7 +635,8 @@ int backward(const ficco_linear_t *op, const void *A, const void *W, const void 
     z.z = (const uint16_t *)pre;
     z.turned = dW ? at(b.dz_turned) : nullptr;
     z.same = dA ? at(b.dz) : nullptr;
-    z.sums = dbias ? (float *)at(b.sums) : nullptr;
+    const bool one_block = M <= kTurnRows;                     // its sums are dbias
+    z.sums = !dbias ? nullptr : one_block ? (float *)dbias : (float *)at(b.sums);
     z.R = M; z.Cc = N; z.ld = o.ldc; z.ldz = o.ld_pre; z.ldt = b.Mp; z.lds = b.Np;
     if (dW && !b.tile_w) {
         ta.src = (const uint16_t *)A;
@@ -593,7 +649,7 @@ int backward(const ficco_linear_t *op, const void *A, const void *W, const void 
         else { tw.turned = at(b.w_other); tw.R = N; tw.Cc = K; tw.ld = K; tw.ldt = b.Np; }
     }
     if ((rc = launch_turn(o.activation, t, s))) return rc;
-    if (dbias && (rc = sum_rows(z.sums, (float *)dbias, (M + kTurnRows - 1) / kTurnRows, N, s))) return rc;
+    if (dbias && !one_block && (rc = sum_rows(z.sums, (float *)dbias, (M + kTurnRows - 1) / kTurnRows, N, s))) return rc;
     const bool own = b.dz >= 0;
     const uint16_t *const dz = own ? at(b.dz) : (const uint16_t *)dC;
     const int64_t ldz = own ? b.Np : o.ldc;

@@ -438,9 +438,11 @@ struct Chunks {
 };
 Chunks chunks_of(const ficco_residual_norm_t &o)
 {
-    // as many as run at once on 256 CUs with 1024 threads each; but a chunk's sums are written and read again, so at least four rows
-    const int64_t target = 256 * 1024 / threads_of(o.width);
-    const int64_t each = std::max<int64_t>(4, (o.rows + target - 1) / target);
+    // as many as run at once on 256 CUs with 1024 threads each; but a chunk's sums are written and read again, so more than 1024 of
+    // them only where each has 16 rows
+    const int64_t most = 256 * 1024 / threads_of(o.width);
+    const int64_t target = std::min(most, std::max<int64_t>(1024, o.rows / 16));
+    const int64_t each = std::max<int64_t>(1, (o.rows + target - 1) / target);
     Chunks c{};
     if (!o.gate_rows || o.gate_rows >= o.rows) {
         c.groups = 1;

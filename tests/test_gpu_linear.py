@@ -81,7 +81,7 @@ def within(got, ref, tol, what):
 
 # one row to more than a tile of each kind, odd ones; k of one k-tile to many; columns that fill no tile and no lane's eight
 SIZES = [(1, 64, 8), (1, 4096, 768), (3, 128, 40), (16, 2112, 264), (17, 64, 520), (33, 512, 72), (64, 4096, 768), (65, 1024, 200), (127, 192, 1032), (300, 576, 1160), (1000, 320, 328),
-         (2311, 128, 2056), (4100, 64, 1544), (530, 8192, 136), (198, 13440, 2392), (1404, 13888, 464)]
+         (2311, 128, 2056), (4100, 64, 1544), (530, 8192, 136), (198, 13440, 2392), (1404, 13888, 464), (9, 8192, 1032), (1, 5120, 1160), (40, 16384, 520), (300, 10624, 456), (16, 2112, 2056)]
 
 
 @pytest.mark.parametrize("kn", [True, False], ids=["kn", "nk"])
