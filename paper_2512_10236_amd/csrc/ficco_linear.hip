@@ -51,7 +51,7 @@ struct RowsCfg {
     static constexpr int RING = D * STAGE, PART = FM * NB * 1024;
     static constexpr int LDS_BYTES = WAVES * (RING > PART ? RING : PART);
     static_assert(D >= 2 && (D - 1) * LOADS < 64, "a ring of two stages or more, vmcnt has 6 bits");
-    static_assert(!SB || NB % 4 == 0, "whole lines of a [K,N] weight's rows");
+    static_assert(!SB || NB == 2 || NB % 4 == 0, "whole lines, or halves, of a [K,N] weight's rows");
 };
 constexpr int kRowsThreads = 512;
 
@@ -211,7 +211,7 @@ int launch_rows_t(const LinearLaunch &a, int splits, float *part, hipStream_t s)
 // Tiles of the few-rows kernel: 8 ab rows x 16 nb columns, of an [N,K] weight or of a [K,N] one
 #define FICCO_FOR_EACH_ROWS(X) \
     X(1, 1, false) X(1, 2, false) X(1, 4, false) X(2, 1, false) X(2, 2, false) X(2, 4, false) X(4, 1, false) X(4, 2, false) X(8, 1, false) \
-    X(1, 4, true) X(2, 4, true)
+    X(1, 2, true) X(2, 2, true) X(1, 4, true) X(2, 4, true)
 int launch_rows(int ab, int nb, bool kn, const LinearLaunch &a, int splits, float *part, hipStream_t s)
 {
 #define X(AB, NB, SB) if (ab == AB && nb == NB && kn == SB) return launch_rows_t<RowsCfg<AB, NB, SB>>(a, splits, part, s);
@@ -248,13 +248,14 @@ RowsTile rows_tile(int64_t M, int64_t K, int64_t N, double us)
     return best;
 }
 
-// The same of a [K,N] weight, against the direct kernel (row_blocks, us: what that would take) or, row_blocks = 0, a tile's us. A workgroup
-// reads 128 bytes of each row of the weight, and k may be split over as many workgroups as make one round, joined by a second launch.
-// Which is the fastest depends on where the weight comes from: a CU draws 146-90 KB a us of it from the L2s and about 42 from memory,
-// whatever the kernel. A loop over one layer finds a weight of up to 16 MiB in the L2s, a model's layers in turn do not; up to there the
-// rule goes by the geometric mean of both. us, direct / one launch / splits (one layer | layers in turn): M 64, K 4096, N 768 9.1 / 7.6 /
-// 9.5 | 15.3 / 14.4 / 11.6; M 1, K 11456, N 72 20.1 / 14.7 / - | -; M 3, K 4800, N 560 - | 20.9 / 22.9 / 11.7; beyond M 16, K 8192, N 3584
-// - | 38 / 36 / 20; M 1, K 8192, N 1280 29 / 31 / 13; M 166, K 13184, N 264 50 / 43 / 19; M 32, K 16384, N 4096 68 / 61 / 42.
+// The same of a [K,N] weight, against the direct kernel (row_blocks, us: what that would take) or, row_blocks = 0, a tile's us. In one
+// launch a workgroup has 32 columns, which puts twice as many CUs to work as 64; or k is split over as many workgroups of 64 columns
+// (whole lines of the weight's rows) as make one round, and a second launch joins them. Which is the fastest depends on where the
+// weight comes from: a CU draws 90-146 KB a us of it from the L2s, and from memory 43, 32 of half lines. A loop over one
+// layer finds a weight of up to 16 MiB in the L2s, a model's layers in turn do not; up to there the rule goes by the geometric mean
+// of both. us, direct / one launch / splits (one layer | layers in turn): M 1, K 4096, N 768 9.0 / 6.5 / 9.0 | 14.5 / 15.8 / 10.3; M 64 of
+// it 9.0 / 7.3 / 9.5 | 15.3 / 14.2 / 11.7; M 3, K 4800, N 560 10.0 / 7.0 / 9.0 | 20.5 / 17.2 / 11.2; beyond 16 MiB M 16, K 8192, N 3584
+// - | 38 / 32 / 20; M 1, K 8192, N 1280 30 / 29 / 13; M 166, K 13184, N 264 50 / - / 19; M 32, K 16384, N 4096 68 / - / 42.
 RowsTile rows_tile_kn(int64_t M, int64_t K, int64_t N, int row_blocks, double us)
 {
     RowsTile best{0, 0, 1};
@@ -268,13 +269,16 @@ RowsTile rows_tile_kn(int64_t M, int64_t K, int64_t N, int row_blocks, double us
     }
     for (int ab = 1; ab <= 2; ++ab) {
         if (ab > 1 && M <= 8) break;
-        const int64_t tiles = ((M + 8 * ab - 1) / (8 * ab)) * ((N + 63) / 64);
-        for (int splits = 1; splits <= 16 && tiles * splits <= cus; splits *= 2) {
+        for (int splits = 1; splits <= 16; splits *= 2) {
+            const int nb = splits > 1 ? 4 : 2;
+            const int64_t workgroups = ((M + 8 * ab - 1) / (8 * ab)) * ((N + 16 * nb - 1) / (16 * nb)) * splits;
             if (splits > 1 && K / kBK < splits * 8) break;             // a k-tile for each wavefront
-            const double kb = (64 + 8 * ab) * (double)K * 2e-3 / splits, drawn = kb / (146.0 - 56.0 * (double)(tiles * splits) / cus);
+            if (workgroups > cus) continue;
+            const double kb = (16 * nb + 8 * ab) * (double)K * 2e-3 / splits;
             const double bytes = (double)(N * K + M * K) * 2 + (splits > 1 ? (double)splits * (double)(M * N) * 8 : 0);
-            const double t = splits > 1 ? both(8.5 + drawn, 8.5 + std::max(kb / 43, bytes / 4.9e6)) : both(3.0 + drawn, 5.0 + std::max(kb / 42, bytes / 4.9e6));
-            if (t < us * (splits > 1 && best.splits == 1 ? 0.9 : 0.97)) { us = t; best = {ab, 4, splits}; }
+            const double t = splits > 1 ? both(8.5 + kb / (146.0 - 56.0 * (double)workgroups / cus), 8.5 + std::max(kb / 43, bytes / 4.9e6))
+                                        : both(3.0 + kb / 93, 5.0 + std::max(kb / 32, bytes / 4.9e6));
+            if (t < us * (splits > 1 && best.splits == 1 ? 0.9 : 0.97)) { us = t; best = {ab, nb, splits}; }
         }
     }
     return best;

@@ -182,7 +182,8 @@ struct KStrided { static constexpr bool STRIDED = true; };
 template <int DIM>
 static __device__ __forceinline__ int strided_swizzle(int row)
 {
-    static_assert(DIM % 64 == 0, "whole lines");
+    static_assert(DIM % 64 == 0 || DIM == 32, "whole lines, or halves of them");
+    if constexpr (DIM == 32) return 2 * ((row >> 3) & 1);      // four rows fill the banks
     return DIM % 128 == 0 ? 2 * ((row & 3) | (((row >> 3) & 1) << 2)) : 2 * (((row >> 1) & 1) | (((row >> 3) & 1) << 1));
 }
 // Byte offset, from the tile's first column of its first row, of what lane `lane` fetches for 1 KiB block `blk` of a stage (columns
