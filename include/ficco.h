@@ -572,8 +572,9 @@ typedef enum ficco_weight_layout {
  * Row strides in elements, 0 = dense: lda of A, ldc of C and of dC, ld_residual, ld_pre; multiples of 8, at least the row's
  * length and at most 2^22. Shape rules (FICCO_ERR_SHAPE): 0 <= M < 2^31, K % 64 == 0, N % 8 == 0, K and N
  * positive and at most 2^22; the backward pass needs M <= 2^22. With M == 0 nothing is read; dW and dbias are zero.
- * Workspace: the forward of a [K,N] weight keeps its re-laid out copy there (K N 2 bytes) unless the product is small; the
- * backward keeps dZ and the operands that its products need with another order of their values.
+ * Workspace: the forward of a [K,N] weight keeps there the partial sums of a long k over few rows, or, where neither such a product nor
+ * one over whole tiles is the fastest, a re-laid out copy of the weight; the backward keeps dZ and the operands that its
+ * products need with another order of their values.
  */
 typedef struct ficco_linear_t {
     int64_t M, K, N;
@@ -602,7 +603,7 @@ int ficco_linear_backward(const ficco_linear_t *op, const void *A, const void *W
  * Gradients, from dy of stream_type (NULL: 0) and dh bf16 (NULL, with dpre_weight: h was not used), with y as stored:
  *   dY = dy + (the norm's part of dh);  dx = residual_scale * dY (stream_type; NULL: not wanted; may be dy itself)
  *   dblock bf16, and fp32 sums over the rows: dpost_weight [width], dgate of the gate's shape, dpre_weight [width]
- * each given or NULL; those of NULL parameters must be NULL. dblock and dgate need block (FICCO_ERR_ARG).
+ * each given or NULL; those of NULL parameters must be NULL. dpost_weight, dgate and, with post_weight, dblock need block (FICCO_ERR_ARG).
  * Shape rules (FICCO_ERR_SHAPE): 0 <= rows < 2^31, width % 8 == 0, 8 <= width <= 16384, gate_rows >= 0. With no rows
  * nothing is read, and the sums are zero. eps >= 0 and finite (FICCO_ERR_ARG).
  */
@@ -636,7 +637,7 @@ int ficco_residual_norm_backward(const ficco_residual_norm_t *op, const void *y,
  * The gradient: dlogits of logits' type and stride = dloss[0] (fp32, NULL: 1) times d loss / d logits, through the
  * probabilities (counts are constants); 0 for padding. It takes counts and group_valid as the forward wrote them. dlogits may be logits itself.
  * Shape rules (FICCO_ERR_SHAPE): 0 <= tokens < 2^31, 1 <= experts <= 1024, 1 <= top_k <= 64, group_tokens >= 0, at most
- * 2^20 groups. With no tokens there are no groups: the loss is 0 and nothing else is written.
+ * 2^20 groups and 2^31 - 1 slots in each. With no tokens there are no groups: the loss is 0 and nothing else is written.
  */
 typedef struct ficco_expert_balance_t {
     int64_t tokens, group_tokens, ld_logits;

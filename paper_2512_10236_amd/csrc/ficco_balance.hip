@@ -316,6 +316,7 @@ int checked(const ficco_expert_balance_t *op, ficco_expert_balance_t *out)
     if (o.logits_type < FICCO_BF16 || o.logits_type > FICCO_F32 || !std::isfinite(o.coefficient)) return FICCO_ERR_ARG;
     if (o.tokens < 0 || o.tokens > 0x7FFFFFFF || o.experts < 1 || o.experts > 1024 || o.top_k < 1 || o.top_k > 64 || o.group_tokens < 0) return FICCO_ERR_SHAPE;
     if (!o.group_tokens || o.group_tokens > o.tokens) o.group_tokens = std::max<int64_t>(o.tokens, 1);
+    if (o.group_tokens * o.top_k > 0x7FFFFFFF) return FICCO_ERR_SHAPE;       // a count's 32 bits
     if ((o.tokens + o.group_tokens - 1) / o.group_tokens > (1 << 20)) return FICCO_ERR_SHAPE;
     if (!o.ld_logits) o.ld_logits = o.experts;
     if (o.ld_logits < o.experts || o.ld_logits > kMaxK) return FICCO_ERR_SHAPE;

@@ -237,6 +237,7 @@ RowsTile rows_tile(int64_t M, int64_t K, int64_t N, double us)
     auto consider = [&](int ab, int nb) {
         if (ab > 1 && M <= 8 * ab / 2) return;                 // half of the rows or more would not be there
         const int64_t tiles = ((M + 8 * ab - 1) / (8 * ab)) * ((N + 16 * nb - 1) / (16 * nb)), full = tiles / cus, rest = tiles - full * cus;
+        if (tiles > 0x7FFFFFFF / kRowsThreads) return;         // threads of a launch
         const double kb = (16 * nb + 8 * ab) * (double)K * 2e-3;
         const double drawn = (double)full * kb / 90 + (rest ? kb / (146.0 - 56.0 * (double)rest / cus) : 0) + 2.5 * (double)((tiles + cus - 1) / cus - 1);
         const double t = 3.0 + std::max(drawn, (double)(N * K + M * K) * 2 / 7.3e6);
@@ -485,7 +486,8 @@ Forward forward_way(const ficco_linear_t &o)
     double us = 0;
     f.tile = tile_for(o.M, o.K, o.N, &us);
     if (o.weight_layout == FICCO_WEIGHT_KN) {
-        if (o.K * o.N * 2 <= 0x7FFFFFFF) f.row_blocks = direct_row_blocks(o.M, o.K, o.N, compute_units(), us, &us);
+        // the direct kernel's offsets have 32 bits, and so has its launch's number of threads
+        if (o.K * o.N * 2 <= 0x7FFFFFFF && (o.M + 15) / 16 * ((o.N + 63) / 64) <= 0x7FFFFFFF / 256) f.row_blocks = direct_row_blocks(o.M, o.K, o.N, compute_units(), us, &us);
         f.rows = rows_tile_kn(o.M, o.K, o.N, f.row_blocks, us);
         if (f.rows.ab) f.row_blocks = 0;
         else if (!f.row_blocks && !strided_tile(f.tile, false)) f.bytes = round_up(o.K * o.N * 2, 256);

@@ -304,7 +304,7 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), (V == 1 ? 4 : 2)) void r
         }
         if (KEEP && row + 1 < end) load(next, row + 1, 0);
         thread_sums<TPR, 3>(s, s_a[parity]);
-        const float r = rsqrtf(fmaf(s[0], inv, a.eps)), back = r * r * r * s[1] * inv;
+        const float r = rsqrtf(fmaf(s[0], inv, a.eps)), back = r * (r * (r * s[1] * inv));   // r^3 alone may be past fp32's range
         const float rb = post ? rsqrtf(fmaf(s[2], inv, a.eps)) : 1.0f;
         float s4[1] = {0.f};
 #pragma unroll
@@ -354,7 +354,7 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), (V == 1 ? 4 : 2)) void r
         }
         if (post) thread_sums<TPR, 1>(s4, s_b[parity]);
         if (a.h) {
-            const float back_b = rb * rb * rb * s4[0] * inv;
+            const float back_b = rb * (rb * (rb * s4[0] * inv));
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 if (post) {
@@ -540,7 +540,7 @@ int backward(const ficco_residual_norm_t *op, const void *y, const void *block, 
     if (rc) return rc;
     const bool none = o.rows == 0, sums = dpost || dgate || dpre;
     if ((dpost && !post) || (dgate && !gate) || (dpre && !pre) || (dpre && !dh && !none) || (dh && !pre)) return FICCO_ERR_ARG;
-    const bool needs_block = post || dgate;
+    const bool needs_block = dpost || dgate || (dblock && post);
     rc = check_args({{y, 16, none || !dh}, {block, 16, none || !needs_block}, {post, 16, true}, {gate, 16, true}, {pre, 16, true}, {dy, 16, true}, {dh, 16, true},
                      {dx, 16, true}, {dblock, 16, true}, {dpost, 16, true}, {dgate, 16, true}, {dpre, 16, true}, {workspace, 16, none || !sums}});
     if (rc) return rc;
@@ -552,7 +552,7 @@ int backward(const ficco_residual_norm_t *op, const void *y, const void *block, 
     if (dgate && !c.whole_groups && (!none || !op->gate_rows)) { t.dgate = (float *)dgate; groups = (int)c.groups; }
     if (!none) {
         NormLaunch a{};
-        a.x = y; a.block = needs_block ? (const uint16_t *)block : nullptr; a.post = post; a.gate = gate; a.pre = pre;
+        a.x = y; a.block = needs_block ? (const uint16_t *)block : nullptr; a.post = needs_block ? post : nullptr; a.gate = gate; a.pre = pre;
         a.y = dx; a.h = (uint16_t *)dblock; a.dy = dy; a.dh = (const uint16_t *)dh;
         a.sums = (float *)workspace;
         a.dgate = c.whole_groups ? (float *)dgate : nullptr;

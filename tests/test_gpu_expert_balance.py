@@ -192,3 +192,18 @@ def test_refusals_on_the_device(gpu):
         with pytest.raises(F.FiccoError) as e:
             F.ficco_expert_balance(c.op, *args, gpu["cs"])
         assert e.value.status == F.FICCO_ERR_ARG
+
+
+def test_rows_whose_offsets_pass_32_bits(gpu):
+    """2^32 values from the first row to the last; the last group's results are those of the group by itself, but for the share that
+    a group has in the loss, a power of two here."""
+    groups, size = 1024, 4096
+    c = Case(gpu, groups * size, 64, 4, group=size, logits="bf16", ld=1024)
+    c.forward()
+    one = Case(gpu, size, 64, 4, logits="bf16")
+    one.logits.copy_(c.logits[-size:])
+    one.ids = c.ids[-size:].clone()
+    one.op.coefficient /= groups
+    one.forward()
+    assert torch.equal(c.counts[groups - 1], one.counts[0]) and c.group_valid[groups - 1] == size
+    assert torch.equal(c.backward(in_place=True)[-size:, :64], one.backward())

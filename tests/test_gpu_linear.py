@@ -137,6 +137,28 @@ def test_rows_at_strides_of_their_own(gpu, M, kn):
 
 
 @pytest.mark.parametrize("kn", [True, False], ids=["kn", "nk"])
+@pytest.mark.parametrize("M,K,N", [(512, 4096, 8), (640, 128, 72), (640, 512, 2048)])
+def test_rows_whose_offsets_pass_32_bits(gpu, M, K, N, kn):
+    """All matrices with rows side by side in one buffer whose rows are as far apart as they may be: 4 GiB and more in all."""
+    far = 1 << 22
+    normal = seeded(gpu, M + K)
+    A, W, R, dC = normal(M, K), weight(normal, K, N, kn), normal(M, N), normal(M, N)
+    store = torch.full((M, far), 7.0, dtype=torch.bfloat16, device=gpu["dev"])
+    fA, fC, fpre, fdC = (store[:, at:at + n] for at, n in ((0, K), (8192, N), (16384, N), (24576, N)))
+    fA.copy_(A), fC.copy_(R), fdC.copy_(dC)
+    outs = []
+    for ld, a, c, pre, d in [(0, A, R, torch.empty_like(R), dC), (far, fA, fC, fpre, fdC)]:
+        op = F.ficco_linear_t(M=M, K=K, N=N, weight_layout=int(not kn), activation=F.FICCO_ACT_SILU, lda=ld, ldc=ld, ld_residual=ld, ld_pre=ld)
+        dA, dW, db = torch.empty_like(A), torch.empty_like(W), torch.empty(N, device=gpu["dev"])
+        forward(gpu, op, a, W, None, c, pre, c)
+        backward(gpu, op, a, W, pre, d, dA, dW, db)
+        outs.append((c, pre, dA, dW, db))
+    for x, y in zip(*outs):
+        assert torch.equal(x, y)
+    assert (store[:, 8192 + N:16384] == 7).all() and (store[:, 16384 + N:24576] == 7).all()
+
+
+@pytest.mark.parametrize("kn", [True, False], ids=["kn", "nk"])
 @pytest.mark.parametrize("M,K,N", [(1, 64, 8), (3, 128, 40), (64, 256, 64), (100, 64, 72), (257, 576, 264), (1187, 320, 1160), (70, 2048, 136), (2100, 192, 128)])
 def test_backward(gpu, M, K, N, kn):
     normal = seeded(gpu, M * 5 + K + N)

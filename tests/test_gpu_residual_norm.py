@@ -218,6 +218,52 @@ def test_rows_of_zeros_and_of_nothing_finite(gpu):
     assert torch.isnan(h[5]).all() and torch.isnan(h[6, 9])
 
 
+@pytest.mark.parametrize("width", [520, 8200])
+def test_rows_of_zeros_with_a_tiny_eps(gpu, width):
+    """1 / sqrt(eps) = 1e15 there, whose cube is past fp32's range; the gradients are dY = dy + r w dh and db = r p g dY."""
+    c = Case(gpu, 6, width, stream="f32", param="f32")
+    c.op.eps, r = 1e-30, 1e15
+    c.x[3] = 0
+    c.block[3] = 0
+    y, h = c.forward()
+    assert (h[3] == 0).all() and (y[3] == 0).all()
+    out = c.backward(y)
+    dy = c.dy[3].double() + r * c.pre.double() * c.dh[3].double()
+    within(out["dx"][3], c.scale * dy, c.scale * (E + P) * (c.dy[3].abs().double() + r * (c.pre.double() * c.dh[3].double()).abs()), "dx")
+    db = r * c.post.double() * c.gate.double() * dy
+    within(out["dblock"][3], db, (U + 2 * P) * db.abs() + r * P * c.dy[3].abs().double(), "dblock")
+
+
+def test_block_is_only_needed_for_what_it_takes_part_in(gpu):
+    c = Case(gpu, 40, 264, gate_rows=7)
+    y, _ = c.forward()
+    whole, c.block = c.backward(y), None
+    assert torch.equal(c.backward(y, "dx dpre")["dx"], whole["dx"]) and torch.equal(c.backward(y, "dpre")["dpre"], whole["dpre"])
+    for want in ("dblock", "dpost", "dgate"):
+        with pytest.raises(F.FiccoError) as e:
+            c.backward(y, want)
+        assert e.value.status == F.FICCO_ERR_ARG
+    c = Case(gpu, 40, 264, gate_rows=7, post=False)
+    y, _ = c.forward()
+    whole, c.block = c.backward(y), None
+    assert torch.equal(c.backward(y, "dx dblock")["dblock"], whole["dblock"])
+
+
+def test_rows_whose_offsets_pass_32_bits(gpu):
+    """2^31 values and some rows more: the last rows come out as by themselves."""
+    rows, last = (1 << 18) + 12, 12
+    c = Case(gpu, rows, 8192, gate=False)
+    y, h = c.forward()
+    out = c.backward(y, "dx dblock")
+    small = Case(gpu, last, 8192, gate=False)
+    small.post, small.pre = c.post, c.pre
+    small.x, small.block, small.dy, small.dh = (t[rows - last:].clone() for t in (c.x, c.block, c.dy, c.dh))
+    y1, h1 = small.forward()
+    one = small.backward(y1, "dx dblock")
+    for big, little in ((y, y1), (h, h1), (out["dx"], one["dx"]), (out["dblock"], one["dblock"])):
+        assert torch.equal(big[rows - last:rows], little[:last])
+
+
 def test_no_rows(gpu):
     for gate_rows in (0, 4):
         op = F.ficco_residual_norm_t(rows=0, width=64, gate_rows=gate_rows, residual_scale=1.0, eps=EPS)

@@ -120,7 +120,7 @@ def balance(**k):
 
 
 @pytest.mark.parametrize("bad", [dict(tokens=-1), dict(tokens=1 << 31), dict(experts=0), dict(experts=1025), dict(top_k=0), dict(top_k=65), dict(group_tokens=-1), dict(ld_logits=3),
-                                 dict(tokens=(1 << 20) + 1, group_tokens=1)])
+                                 dict(tokens=(1 << 20) + 1, group_tokens=1), dict(tokens=(1 << 31) - 1, top_k=2), dict(tokens=1 << 30, group_tokens=1 << 28, top_k=8)])
 def test_balance_shapes(bad):
     assert set(balance(**bad)) == {F.FICCO_ERR_SHAPE}
 
