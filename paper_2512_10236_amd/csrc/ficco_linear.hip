@@ -252,11 +252,13 @@ RowsTile rows_tile(int64_t M, int64_t K, int64_t N, double us)
 // The same of a [K,N] weight, against the direct kernel (row_blocks, us: what that would take) or, row_blocks = 0, a tile's us. In one
 // launch a workgroup has 32 columns, which puts twice as many CUs to work as 64; or k is split over as many workgroups of 64 columns
 // (whole lines of the weight's rows) as make one round, and a second launch joins them. Which is the fastest depends on where the
-// weight comes from: a CU draws 90-146 KB a us of it from the L2s, and from memory 43, 32 of half lines. A loop over one
+// weight comes from: a CU draws 90-146 KB a us of it from the L2s (40-105 of half lines, the fewer the more CUs do), and from memory 43 (32). A loop over one
 // layer finds a weight of up to 16 MiB in the L2s, a model's layers in turn do not; up to there the rule goes by the geometric mean
 // of both. us, direct / one launch / splits (one layer | layers in turn): M 1, K 4096, N 768 9.0 / 6.5 / 9.0 | 14.5 / 15.8 / 10.3; M 64 of
 // it 9.0 / 7.3 / 9.5 | 15.3 / 14.2 / 11.7; M 3, K 4800, N 560 10.0 / 7.0 / 9.0 | 20.5 / 17.2 / 11.2; beyond 16 MiB M 16, K 8192, N 3584
 // - | 38 / 32 / 20; M 1, K 8192, N 1280 30 / 29 / 13; M 166, K 13184, N 264 50 / - / 19; M 32, K 16384, N 4096 68 / - / 42.
+// Over 110 random products (M to 500, K 1024-16384, N 64-6144) what it takes is 1.4 % slower than the fastest; the direct kernel or a tile
+// throughout 42 %.
 RowsTile rows_tile_kn(int64_t M, int64_t K, int64_t N, int row_blocks, double us)
 {
     RowsTile best{0, 0, 1};
@@ -278,7 +280,7 @@ RowsTile rows_tile_kn(int64_t M, int64_t K, int64_t N, int row_blocks, double us
             const double kb = (16 * nb + 8 * ab) * (double)K * 2e-3 / splits;
             const double bytes = (double)(N * K + M * K) * 2 + (splits > 1 ? (double)splits * (double)(M * N) * 8 : 0);
             const double t = splits > 1 ? both(8.5 + kb / (146.0 - 56.0 * (double)workgroups / cus), 8.5 + std::max(kb / 43, bytes / 4.9e6))
-                                        : both(3.0 + kb / 93, 5.0 + std::max(kb / 32, bytes / 4.9e6));
+                                        : both(3.0 + kb / (105.0 - 65.0 * (double)workgroups / cus), 5.0 + std::max(kb / 32, bytes / 4.9e6));
             if (t < us * (splits > 1 && best.splits == 1 ? 0.9 : 0.97)) { us = t; best = {ab, nb, splits}; }
         }
     }
