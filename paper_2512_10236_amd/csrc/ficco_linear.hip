@@ -225,19 +225,20 @@ int launch_rows(int ab, int nb, bool kn, const LinearLaunch &a, int splits, floa
 // CU holds one workgroup; and a launch cannot be faster than the weight's way through the chip, 7.3 TB/s if it is cached.
 // Fitted to M 1-256 of eight shapes, K 512-16384, N 64-14336, each tile forced in turn (us, the other kernels / the tile taken:
 // M 16, K 8192, N 3584 29.6 / 11.6; M 64 29.9 / 14.9; M 128 29.7 / 25.5; M 256 32.3, its best tile 48.9; M 64, K 4096, N 768 11.8 /
-// 5.5; M 16, K 8192, N 64 18.8 / 5.9; M 64, K 4096, N 14336 21.6, its best tile 32.3).
+// 5.5; M 16, K 8192, N 64 18.8 / 5.9; M 64, K 4096, N 14336 21.6, its best tile 32.3). More rows pay where the columns are few, in one or
+// two rounds: M 534, K 3584, N 432 14.0 / 8.9, M 1222, K 8896, N 192 33.2 / 22.4; not in three, M 1456, K 9856, N 432 41.5 / 68.3.
 struct RowsTile {
     int ab, nb, splits;
 };
 RowsTile rows_tile(int64_t M, int64_t K, int64_t N, double us)
 {
     RowsTile best{0, 0, 1};
-    if (M > 512) return best;
+    if (M > 2048) return best;
     const int cus = compute_units();
     auto consider = [&](int ab, int nb) {
         if (ab > 1 && M <= 8 * ab / 2) return;                 // half of the rows or more would not be there
         const int64_t tiles = ((M + 8 * ab - 1) / (8 * ab)) * ((N + 16 * nb - 1) / (16 * nb)), full = tiles / cus, rest = tiles - full * cus;
-        if (tiles > 0x7FFFFFFF / kRowsThreads) return;         // threads of a launch
+        if (tiles > (M > 512 ? 2 * cus : 0x7FFFFFFF / kRowsThreads)) return;       // ... or threads of a launch
         const double kb = (16 * nb + 8 * ab) * (double)K * 2e-3;
         const double drawn = (double)full * kb / 90 + (rest ? kb / (146.0 - 56.0 * (double)rest / cus) : 0) + 2.5 * (double)((tiles + cus - 1) / cus - 1);
         const double t = 3.0 + std::max(drawn, (double)(N * K + M * K) * 2 / 7.3e6);
@@ -481,31 +482,54 @@ struct Forward {
     RowsTile rows;
     int64_t bytes;
 };
-Forward forward_way(const ficco_linear_t &o)
+Forward forward_way(int64_t M, int64_t K, int64_t N, bool kn)
 {
     Forward f{};
-    if (o.M == 0) return f;
+    if (M == 0) return f;
     double us = 0;
-    f.tile = tile_for(o.M, o.K, o.N, &us);
-    if (o.weight_layout == FICCO_WEIGHT_KN) {
+    f.tile = tile_for(M, K, N, &us);
+    if (kn) {
         // the direct kernel's offsets have 32 bits, and so has its launch's number of threads
-        if (o.K * o.N * 2 <= 0x7FFFFFFF && (o.M + 15) / 16 * ((o.N + 63) / 64) <= 0x7FFFFFFF / 256) f.row_blocks = direct_row_blocks(o.M, o.K, o.N, compute_units(), us, &us);
-        f.rows = rows_tile_kn(o.M, o.K, o.N, f.row_blocks, us);
+        if (K * N * 2 <= 0x7FFFFFFF && (M + 15) / 16 * ((N + 63) / 64) <= 0x7FFFFFFF / 256) f.row_blocks = direct_row_blocks(M, K, N, compute_units(), us, &us);
+        f.rows = rows_tile_kn(M, K, N, f.row_blocks, us);
         if (f.rows.ab) f.row_blocks = 0;
-        else if (!f.row_blocks && !strided_tile(f.tile, false)) f.bytes = round_up(o.K * o.N * 2, 256);
+        else if (!f.row_blocks && !strided_tile(f.tile, false)) f.bytes = round_up(K * N * 2, 256);
     } else {
-        f.rows = rows_tile(o.M, o.K, o.N, us);
+        f.rows = rows_tile(M, K, N, us);
     }
-    if (f.rows.ab && f.rows.splits > 1) f.bytes = round_up(f.rows.splits * o.M * o.N * 4, 256);
+    if (f.rows.ab && f.rows.splits > 1) f.bytes = round_up(f.rows.splits * M * N * 4, 256);
     return f;
 }
 
-// How a backward goes: the tiles of the products that read their operands as they are (0: they are turned first), and the
-// workspace, in bytes from its start (-1: not needed).
+int run(const Forward &f, bool kn, LinearLaunch a, void *workspace, hipStream_t s)
+{
+    if (f.row_blocks) {
+        DirectLaunch d{};
+        d.A = a.A;
+        d.W = a.W;
+        d.C = a.C;
+        d.M = a.M; d.N = a.N; d.K = a.K;
+        HIP_TRY(launch_direct_epilogue(f.row_blocks, d, a.e, a.lda, a.ldc, s));
+        return FICCO_OK;
+    }
+    if (f.rows.ab) return launch_rows(f.rows.ab, f.rows.nb, kn, a, f.rows.splits, (float *)workspace, s);
+    if (kn && !f.bytes) return launch_tiles_strided(strided_tile(f.tile, false), false, a, s);
+    if (kn) {
+        HIP_TRY(launch_pack_weight(a.W, (uint16_t *)workspace, a.K, a.N, s));
+        a.W = (const uint16_t *)workspace;
+        a.ldw = a.K;
+    }
+    return launch_tiles(f.tile, a, s);
+}
+
+// How a backward goes, and the workspace, in bytes from its start (-1: not needed). dA is a forward product of dZ with W as a weight
+// of the other layout. dW = A^T dZ has a tile of the kernel that reads A as it is (0: A is turned first).
 struct Backward {
     int64_t Mp, Np;               // M and N rounded up to whole k-tiles
-    int tile_a, tile_w;
-    int64_t dz, dz_turned, a_turned, w_other, sums, bytes;
+    Forward a;
+    bool a_kn;
+    int tile_w;
+    int64_t dz, dz_turned, a_turned, w_other, part, sums, bytes;
 };
 Backward backward_way(const ficco_linear_t &o)
 {
@@ -516,7 +540,12 @@ Backward backward_way(const ficco_linear_t &o)
     const bool kn = o.weight_layout == FICCO_WEIGHT_KN;
     // dA = dZ W^T sums over n, and an [N,K] weight has k next to each other; dW = A^T dZ sums over m, and A has k next to each other. What
     // lies behind the last n or m must be zero, which only a copy is.
-    if (!kn && b.Np == o.N) b.tile_a = strided_tile(tile_for(o.M, b.Np, o.K, nullptr), false);
+    b.a_kn = !kn && b.Np == o.N;
+    if (b.a_kn) {
+        b.a = forward_way(o.M, b.Np, o.K, true);
+        if (b.a.bytes && !b.a.rows.ab) b.a_kn = false;         // a copy: made with the others
+    }
+    if (!b.a_kn) b.a = forward_way(o.M, b.Np, o.K, false);
     if (b.Mp == o.M) b.tile_w = strided_tile(tile_for(kn ? o.K : o.N, b.Mp, kn ? o.N : o.K, nullptr), kn);
     int64_t at = 0;
     auto take = [&](bool needed, int64_t bytes) {
@@ -527,7 +556,8 @@ Backward backward_way(const ficco_linear_t &o)
     b.dz = take(o.activation != FICCO_ACT_NONE || b.Np != o.N, o.M * b.Np * 2);
     b.dz_turned = take(true, o.N * b.Mp * 2);
     b.a_turned = take(!b.tile_w, o.K * b.Mp * 2);
-    b.w_other = take(!b.tile_a && (!kn || b.Np != o.N), o.K * b.Np * 2);
+    b.w_other = take(!b.a_kn && (!kn || b.Np != o.N), o.K * b.Np * 2);
+    b.part = take(b.a.bytes > 0, b.a.bytes);
     b.sums = take(true, (o.M + kTurnRows - 1) / kTurnRows * o.N * 4);
     b.bytes = at;
     return b;
@@ -589,29 +619,12 @@ int forward(const ficco_linear_t *op, const void *A, const void *W, const void *
     const bool none = o.M == 0;
     rc = check_args({{A, 16, none}, {W, 16, none}, {bias, o.bias_type == FICCO_F32 ? 4 : 2, true}, {residual, 16, true}, {pre, 16, true}, {C, 16, none}, {workspace, 16, true}});
     if (rc || none) return rc;
-    const Forward f = forward_way(o);
+    const Forward f = forward_way(o.M, o.K, o.N, o.weight_layout == FICCO_WEIGHT_KN);
     if (f.bytes > 0 && (!workspace || workspace_bytes < f.bytes)) return FICCO_ERR_ARG;
-    Epilogue e{bias, (const uint16_t *)residual, (uint16_t *)pre, o.ld_residual, o.ld_pre, o.activation, o.bias_type == FICCO_F32};
-    if (f.row_blocks) {
-        DirectLaunch d{};
-        d.A = (const uint16_t *)A;
-        d.W = (const uint16_t *)W;
-        d.C = (uint16_t *)C;
-        d.M = (int32_t)o.M; d.N = (int32_t)o.N; d.K = (int32_t)o.K;
-        HIP_TRY(launch_direct_epilogue(f.row_blocks, d, e, o.lda, o.ldc, s));
-        return FICCO_OK;
-    }
-    LinearLaunch a{(const uint16_t *)A, (const uint16_t *)W, (uint16_t *)C, o.lda, o.K, o.ldc, (int32_t)o.M, (int32_t)o.N, (int32_t)o.K, 0, e};
+    const Epilogue e{bias, (const uint16_t *)residual, (uint16_t *)pre, o.ld_residual, o.ld_pre, o.activation, o.bias_type == FICCO_F32};
     const bool kn = o.weight_layout == FICCO_WEIGHT_KN;
-    if (kn) a.ldw = o.N;
-    if (f.rows.ab) return launch_rows(f.rows.ab, f.rows.nb, kn, a, f.rows.splits, (float *)workspace, s);
-    if (kn) {
-        if (!f.bytes) return launch_tiles_strided(strided_tile(f.tile, false), false, a, s);
-        HIP_TRY(launch_pack_weight((const uint16_t *)W, (uint16_t *)workspace, o.K, o.N, s));
-        a.W = (const uint16_t *)workspace;
-        a.ldw = o.K;
-    }
-    return launch_tiles(f.tile, a, s);
+    return run(f, kn, LinearLaunch{(const uint16_t *)A, (const uint16_t *)W, (uint16_t *)C, o.lda, kn ? o.N : o.K, o.ldc, (int32_t)o.M, (int32_t)o.N, (int32_t)o.K, 0, e},
+               workspace, s);
 }
 
 int backward(const ficco_linear_t *op, const void *A, const void *W, const void *pre, const void *dC, void *dA, void *dW, void *dbias, void *workspace,
@@ -662,8 +675,9 @@ int backward(const ficco_linear_t *op, const void *A, const void *W, const void 
     const uint16_t *const dz = own ? at(b.dz) : (const uint16_t *)dC;
     const int64_t ldz = own ? b.Np : o.ldc;
     if (dA) {
-        if (b.tile_a) rc = product_strided(b.tile_a, false, M, b.Np, K, dz, ldz, (const uint16_t *)W, K, (uint16_t *)dA, s);
-        else rc = product(M, b.Np, K, dz, ldz, b.w_other >= 0 ? at(b.w_other) : (const uint16_t *)W, (uint16_t *)dA, s);
+        const uint16_t *const w = b.w_other >= 0 ? at(b.w_other) : (const uint16_t *)W;
+        if (!b.a_kn && !b.a.rows.ab) rc = product(M, b.Np, K, dz, ldz, w, (uint16_t *)dA, s);
+        else rc = run(b.a, b.a_kn, LinearLaunch{dz, w, (uint16_t *)dA, ldz, b.a_kn ? K : b.Np, K, (int32_t)M, (int32_t)K, (int32_t)b.Np, 0, {}}, at(b.part), s);
         if (rc) return rc;
     }
     if (dW) {
@@ -692,7 +706,7 @@ int ficco_linear_workspace(const ficco_linear_t *op, int backward, int64_t *byte
         if (!bytes) return (int)FICCO_ERR_ARG;
         const int rc = checked(op, backward != 0, &o);
         if (rc) return rc;
-        *bytes = backward ? backward_way(o).bytes : forward_way(o).bytes;
+        *bytes = backward ? backward_way(o).bytes : forward_way(o.M, o.K, o.N, o.weight_layout == FICCO_WEIGHT_KN).bytes;
         return (int)FICCO_OK;
     });
 }

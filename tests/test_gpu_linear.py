@@ -159,7 +159,8 @@ def test_rows_whose_offsets_pass_32_bits(gpu, M, K, N, kn):
 
 
 @pytest.mark.parametrize("kn", [True, False], ids=["kn", "nk"])
-@pytest.mark.parametrize("M,K,N", [(1, 64, 8), (3, 128, 40), (64, 256, 64), (100, 64, 72), (257, 576, 264), (1187, 320, 1160), (70, 2048, 136), (2100, 192, 128)])
+@pytest.mark.parametrize("M,K,N", [(1, 64, 8), (3, 128, 40), (64, 256, 64), (100, 64, 72), (257, 576, 264), (1187, 320, 1160), (70, 2048, 136), (2100, 192, 128), (1, 768, 4096), (3, 512, 8192), (48, 1280, 10624),
+                                   (40, 2048, 520), (600, 192, 8896), (2, 7168, 640), (9, 576, 16384)])
 def test_backward(gpu, M, K, N, kn):
     normal = seeded(gpu, M * 5 + K + N)
     A, W, dC, z = normal(M, K), weight(normal, K, N, kn), normal(M, N), normal(M, N, std=1.5)
