@@ -231,36 +231,54 @@ __global__ __launch_bounds__(256) void balance_kernel(BalanceLaunch a)
     }
 }
 
-// The chunks' results of group blockIdx.x for 64 experts from 64 blockIdx.y on; 16 wavefronts take every 16th chunk.
+// The chunks' results of group blockIdx.x for 64 experts from 64 blockIdx.y on, and 64 gridDim.y further, ...; 16 wavefronts take every
+// 16th chunk, eight of theirs at a time (a chunk that is not there: the last, of which nothing is added).
 __global__ __launch_bounds__(1024) void balance_group_kernel(BalanceLaunch a)
 {
     __shared__ float s_p[16][64];
     __shared__ int s_c[16][64], s_n;
-    const int E = a.experts, group = blockIdx.x, lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6), e = blockIdx.y * 64 + lane;
+    const int E = a.experts, group = blockIdx.x, lane = threadIdx.x & 63, wave = scalar(threadIdx.x >> 6);
     if (threadIdx.x == 0) s_n = 0;
     __syncthreads();
     int n = 0;
     for (int c = threadIdx.x; c < a.per_group; c += 1024) n += a.part_n[group * a.per_group + c];
     if (n) atomicAdd(&s_n, n);
-    float t = 0.f;
-    int count = 0;
-    if (e < E)
-#pragma unroll 4
-        for (int c = wave; c < a.per_group; c += 16) {
-            const int64_t at = ((int64_t)group * a.per_group + c) * E + e;
-            count += a.part_c[at];
-            if (a.loss) t += a.part_p[at];
-        }
-    s_p[wave][lane] = t;
-    s_c[wave][lane] = count;
-    __syncthreads();
-    if (wave) return;
+    float term = 0.f;
+    for (int slab = blockIdx.y; slab * 64 < E; slab += gridDim.y) {
+        const int e = slab * 64 + lane;
+        const int64_t first = (int64_t)group * a.per_group * E + min(e, E - 1);
+        float t = 0.f;
+        int count = 0;
+        for (int c = wave; c < a.per_group; c += 128) {
+            int pc[8];
+            float pt[8];
 #pragma unroll
-    for (int k = 1; k < 16; ++k) { t += s_p[k][lane]; count += s_c[k][lane]; }
-    if (e < E) a.counts[(int64_t)group * E + e] = count;
+            for (int k = 0; k < 8; ++k) {
+                const int64_t at = first + (int64_t)min(c + 16 * k, a.per_group - 1) * E;
+                pc[k] = a.part_c[at];
+                pt[k] = a.loss ? a.part_p[at] : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (c + 16 * k < a.per_group) { count += pc[k]; t += pt[k]; }
+        }
+        __syncthreads();                   // the slab before is done with
+        s_p[wave][lane] = t;
+        s_c[wave][lane] = count;
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int k = 1; k < 16; ++k) { t += s_p[k][lane]; count += s_c[k][lane]; }
+            if (e < E) {
+                a.counts[(int64_t)group * E + e] = count;
+                term += (float)count * t;
+            }
+        }
+    }
+    if (wave) return;
     if (threadIdx.x == 0 && blockIdx.y == 0) a.group_valid[group] = s_n;
     if (a.loss) {
-        const float sum = lane_sum<64>((float)count * t);
+        const float sum = lane_sum<64>(term);
         if (threadIdx.x == 0) (a.n_terms == 1 ? a.loss : a.terms + (int64_t)group * gridDim.y + blockIdx.y)[0] = sum * group_scale(a, s_n);
     }
 }
@@ -327,18 +345,33 @@ int checked(const ficco_expert_balance_t *op, ficco_expert_balance_t *out)
 int lanes_of(int experts) { return experts <= 8 ? 8 : experts <= 16 ? 16 : experts <= 32 ? 32 : 64; }
 
 struct Chunks {
-    int64_t groups, per_group, tokens;
+    int64_t groups, per_group, tokens, joins;      // joins: workgroups that join a group's chunks
 };
-// Chunks for about four workgroups a CU of 256 CUs; a group whose tokens a workgroup takes in 32 turns or fewer is one chunk,
-// which spares the launches that join them.
-Chunks chunks_of(const ficco_expert_balance_t &o)
+void cut(const ficco_expert_balance_t &o, Chunks &c, int64_t per_group)
+{
+    c.per_group = std::max<int64_t>(1, std::min(per_group, o.group_tokens));
+    c.tokens = (o.group_tokens + c.per_group - 1) / c.per_group;
+}
+// A group whose tokens a workgroup takes in 24 turns or fewer is one chunk, which spares the launches that join them. Else the time
+// is that of a chunk's turns and, for the join, that of the number of chunks: least at the root of their product, up to four
+// workgroups a CU of 256 CUs. us (tokens x experts, chunks of one group): 41825 x 22 64 31.2, 256 14.5, 512 13.1, 1024 19.3; 3000 x 64 32 14.1,
+// 128 10.5, 512 12.0; 65536 x 256 256 31.6, 512 25.3, 1024 29.7.
+Chunks forward_chunks(const ficco_expert_balance_t &o)
 {
     Chunks c{};
     c.groups = (o.tokens + o.group_tokens - 1) / o.group_tokens;
-    const int64_t turn = 256 / lanes_of(o.experts);
-    const int64_t each = std::max((o.tokens + 1023) / 1024, turn);
-    c.per_group = o.group_tokens <= 32 * turn ? 1 : (o.group_tokens + each - 1) / each;
-    c.tokens = (o.group_tokens + c.per_group - 1) / c.per_group;
+    const int64_t turn = 256 / lanes_of(o.experts), turns = (o.group_tokens + turn - 1) / turn;
+    cut(o, c, turns <= 24 ? 1 : std::min((int64_t)sqrt(24.0 * (double)turns), std::max<int64_t>(1, 1024 / c.groups)));
+    c.joins = c.groups == 1 && o.experts <= 256 && c.per_group <= 128 ? 1 : (o.experts + 63) / 64;      // one: no launch for the loss
+    return c;
+}
+// The backward joins nothing: about four workgroups a CU of 256 CUs.
+Chunks backward_chunks(const ficco_expert_balance_t &o)
+{
+    Chunks c{};
+    c.groups = (o.tokens + o.group_tokens - 1) / o.group_tokens;
+    const int64_t each = std::max((o.tokens + 1023) / 1024, (int64_t)256 / lanes_of(o.experts));
+    cut(o, c, (o.group_tokens + each - 1) / each);
     return c;
 }
 
@@ -347,7 +380,7 @@ struct Workspace {
 };
 Workspace workspace_of(const ficco_expert_balance_t &o)
 {
-    const Chunks c = chunks_of(o);
+    const Chunks c = forward_chunks(o);
     Workspace w{};
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -360,7 +393,7 @@ Workspace workspace_of(const ficco_expert_balance_t &o)
         w.c = take(c.groups * c.per_group * o.experts * 4);
         w.n = take(c.groups * c.per_group * 4);
     }
-    w.n_terms = c.groups * (c.per_group > 1 ? (o.experts + 63) / 64 : 1);
+    w.n_terms = c.groups * (c.per_group > 1 ? c.joins : 1);
     if (w.n_terms > 1) w.terms = take(w.n_terms * 4);
     w.bytes = at;
     return w;
@@ -421,7 +454,7 @@ int forward(const ficco_expert_balance_t *op, const void *logits, const void *id
         HIP_TRY(hipGetLastError());
         return FICCO_OK;
     }
-    const Chunks c = chunks_of(o);
+    const Chunks c = forward_chunks(o);
     const Workspace w = workspace_of(o);
     if (w.bytes > 0 && (!workspace || workspace_bytes < w.bytes)) return FICCO_ERR_ARG;
     unsigned char *const ws = (unsigned char *)workspace;
@@ -440,7 +473,7 @@ int forward(const ficco_expert_balance_t *op, const void *logits, const void *id
     rc = o.logits_type == FICCO_F32 ? launch<float>(a, false, s) : launch<uint16_t>(a, false, s);
     if (rc) return rc;
     if (c.per_group > 1) {
-        hipLaunchKernelGGL(balance_group_kernel, dim3((unsigned)c.groups, (unsigned)((o.experts + 63) / 64)), dim3(1024), 0, s, a);
+        hipLaunchKernelGGL(balance_group_kernel, dim3((unsigned)c.groups, (unsigned)c.joins), dim3(1024), 0, s, a);
         HIP_TRY(hipGetLastError());
     }
     if (loss && w.n_terms > 1) {
@@ -460,7 +493,7 @@ int backward(const ficco_expert_balance_t *op, const void *logits, const void *v
     const int align = o.logits_type == FICCO_F32 ? 4 : 2;
     rc = check_args({{logits, align, none}, {valid, 1, true}, {counts, 4, none}, {group_valid, 4, none}, {dloss, 4, true}, {dlogits, align, none}});
     if (rc || none) return rc;
-    BalanceLaunch a = launch_of(o, chunks_of(o));
+    BalanceLaunch a = launch_of(o, backward_chunks(o));
     a.logits = logits;
     a.valid = (const uint8_t *)valid;
     a.counts = (int32_t *)const_cast<void *>(counts);

@@ -137,7 +137,7 @@ def test_rows_at_strides_of_their_own(gpu, M, kn):
 
 
 @pytest.mark.parametrize("kn", [True, False], ids=["kn", "nk"])
-@pytest.mark.parametrize("M,K,N", [(512, 4096, 8), (640, 128, 72), (640, 512, 2048)])
+@pytest.mark.parametrize("M,K,N", [(512, 4096, 8), (640, 128, 72), (640, 512, 2048), (530, 256, 136)])
 def test_rows_whose_offsets_pass_32_bits(gpu, M, K, N, kn):
     """All matrices with rows side by side in one buffer whose rows are as far apart as they may be: 4 GiB and more in all."""
     far = 1 << 22
