@@ -21,11 +21,11 @@ struct NormLaunch {
     uint16_t *h;                  // forward: h; backward: dblock
     const void *dy;
     const uint16_t *dh;
-    float *sums;                  // backward: [3][chunks][width] partial sums of dpost, dgate, dpre
+    float *sum_post, *sum_gate, *sum_pre;      // backward: [chunks][width] partial sums (of one chunk: the sums), null: not wanted
     float *dgate;                 // backward: rows of dgate that a chunk holds whole groups of, else null
     int32_t rows, width, gate_rows, param_f32;
     int32_t chunks, per_group, chunk_rows;     // backward: chunk c is the (c % per_group)-th run of chunk_rows rows of its group, ...
-    int32_t want_post, want_gate, want_pre;    // ... or, with per_group 0, of all rows
+                                               // ... or, with per_group 0, of all rows
     float scale, eps;
 };
 
@@ -383,10 +383,10 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), (V == 1 ? 4 : 2)) void r
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         if (there[v] != 0.f) {
-            const int64_t plane = (int64_t)a.chunks * a.width, at = (int64_t)chunk * a.width + col[v];
-            if (a.want_post) store8<true>(a.sums, at, total(kept_post, 0, v));
-            if (a.want_gate && !a.dgate) store8<true>(a.sums, plane + at, dgate[v]);
-            if (a.want_pre) store8<true>(a.sums, 2 * plane + at, total(kept_pre, 1, v));
+            const int64_t at = (int64_t)chunk * a.width + col[v];
+            if (a.sum_post) store8<true>(a.sum_post, at, total(kept_post, 0, v));
+            if (a.sum_gate) store8<true>(a.sum_gate, at, dgate[v]);
+            if (a.sum_pre) store8<true>(a.sum_pre, at, total(kept_pre, 1, v));
         }
     }
 }
@@ -442,7 +442,10 @@ Chunks chunks_of(const ficco_residual_norm_t &o)
     // them only where each has 16 rows
     const int64_t most = 256 * 1024 / threads_of(o.width);
     const int64_t target = std::min(most, std::max<int64_t>(1024, o.rows / 16));
-    const int64_t each = std::max<int64_t>(1, (o.rows + target - 1) / target);
+    int64_t each = std::max<int64_t>(1, (o.rows + target - 1) / target);
+    // three rows or fewer in one chunk need no second launch (3 rows of 960, replayed and called: 5.7 and 6.6 us, in chunks of one
+    // 5.6 and 9.0; 4 rows 7.0 and 7.0, 5.6 and 9.1; 3 rows of 7192 11.0, 9.7)
+    if (o.rows <= 3 && o.width <= 4096) each = std::max<int64_t>(1, o.rows);
     Chunks c{};
     if (!o.gate_rows || o.gate_rows >= o.rows) {
         c.groups = 1;
@@ -547,6 +550,7 @@ int backward(const ficco_residual_norm_t *op, const void *y, const void *block, 
     if (sums && workspace_bytes < workspace_of(o)) return FICCO_ERR_ARG;
     if (!dx && !dblock && !sums) return FICCO_OK;
     const Chunks c = chunks_of(o);
+    const bool one = c.chunks == 1;        // its sums are the sums
     SumLaunch t{(const float *)workspace, (float *)dpost, nullptr, (float *)dpre, (int32_t)c.chunks, (int32_t)c.per_group, (int32_t)o.width};
     int groups = 0;
     if (dgate && !c.whole_groups && (!none || !op->gate_rows)) { t.dgate = (float *)dgate; groups = (int)c.groups; }
@@ -554,17 +558,20 @@ int backward(const ficco_residual_norm_t *op, const void *y, const void *block, 
         NormLaunch a{};
         a.x = y; a.block = needs_block ? (const uint16_t *)block : nullptr; a.post = needs_block ? post : nullptr; a.gate = gate; a.pre = pre;
         a.y = dx; a.h = (uint16_t *)dblock; a.dy = dy; a.dh = (const uint16_t *)dh;
-        a.sums = (float *)workspace;
+        const int64_t plane = c.chunks * o.width;
+        float *const ws = (float *)workspace;
+        a.sum_post = one || !dpost ? (float *)dpost : ws;
+        a.sum_gate = c.whole_groups ? nullptr : one || !dgate ? (float *)dgate : ws + plane;
+        a.sum_pre = one || !dpre ? (float *)dpre : ws + 2 * plane;
         a.dgate = c.whole_groups ? (float *)dgate : nullptr;
         a.rows = (int32_t)o.rows; a.width = (int32_t)o.width; a.gate_rows = (int32_t)o.gate_rows;
         a.param_f32 = o.param_type == FICCO_F32;
         a.chunks = (int32_t)c.chunks; a.chunk_rows = (int32_t)c.rows;
         a.per_group = c.groups > 1 ? (int32_t)c.per_group : 0;
-        a.want_post = dpost != nullptr; a.want_gate = dgate != nullptr; a.want_pre = dpre != nullptr;
         a.scale = o.residual_scale; a.eps = o.eps;
         if ((rc = launch_backward(a, o.stream_type == FICCO_F32, s))) return rc;
     }
-    if (dpost || dpre || t.dgate) {
+    if (!one && (dpost || dpre || t.dgate)) {
         hipLaunchKernelGGL(residual_norm_sum_kernel, dim3((unsigned)((o.width + 31) / 32), (unsigned)(2 + groups)), dim3(1024), 0, s, t);
         HIP_TRY(hipGetLastError());
     }

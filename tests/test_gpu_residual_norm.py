@@ -85,7 +85,8 @@ CASES = [dict(rows=1, width=8), dict(rows=1, width=16384), dict(rows=3, width=26
          dict(rows=1100, width=2056, pre=False, stream="f32"), dict(rows=77, width=4096, post=False, gate_rows=10, param="f32"), dict(rows=600, width=4104, stream="f32", param="f32", gate_rows=599),
          dict(rows=520, width=8192, gate_rows=130), dict(rows=9, width=8200, stream="f32"), dict(rows=300, width=16376, gate_rows=7, param="f32"), dict(rows=5000, width=64, gate_rows=3),
          dict(rows=9001, width=72, gate_rows=2000, stream="f32", param="f32"), dict(rows=700, width=512, post=False, gate=False, pre=False), dict(rows=4099, width=128, gate_rows=0, scale=-1.5),
-         dict(rows=5, width=512, gate_rows=9), dict(rows=2500, width=1024, gate_rows=2500)]
+         dict(rows=5, width=512, gate_rows=9), dict(rows=2500, width=1024, gate_rows=2500), dict(rows=2, width=520, gate_rows=1), dict(rows=3, width=2048, gate_rows=2),
+         dict(rows=3, width=4096, stream="f32"), dict(rows=3, width=4104), dict(rows=2, width=64, gate=False, param="f32")]
 
 
 @pytest.mark.parametrize("kind", CASES, ids=lambda k: "-".join(f"{a}{b}" for a, b in k.items()))
