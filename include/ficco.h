@@ -538,7 +538,7 @@ int ficco_gemm_static(int64_t M, int64_t K, int64_t N, const void *A_dev, const 
 /*
  * Operators around the pair: what a layer does next to the products above, on operands that are already in device memory.
  * They need no plan. Options and sizes are in a struct that the caller fills (zero is every field's default) and may keep;
- * nothing is kept between calls, no device memory is allocated, and the work is enqueued on `stream` (hipStream_t), so that
+ * nothing of the operands is kept between calls, no device memory is allocated, and the work is enqueued on `stream` (hipStream_t), so that
  * the caller may capture it into a graph. A workspace is device memory of the caller's, of at least the bytes that the
  * operator's _workspace function gives for the same struct (NULL where that is 0); it holds nothing between calls, and
  * calls that may run at the same time need one each. All matrices are row-major. Every pointer must be device memory of

@@ -361,20 +361,21 @@ def ficco_ideal_overlap_us(t_comm_us, t_gemm_us, n):
 
 
 # ---- operators around the pair: `op` is the struct of the C interface, tensors have to be laid out as it says
-def _addr(x):
-    """Address of a buffer, a tensor or a stream, or None. A tensor's strides are the caller's to describe in `op`: one whose
-    last dimension is not contiguous cannot be."""
-    if x is None:
-        return None
-    try:
-        p = x.data_ptr()
-    except AttributeError:
-        if isinstance(x, int):
-            return x
-        return x.cuda_stream
-    if not x.is_contiguous() and x.stride(-1) != 1 and x.size(-1) > 1:
-        raise FiccoError(FICCO_ERR_ARG, "a tensor's last dimension must be contiguous")
-    return p
+def _addrs(*buffers):
+    """Addresses of buffers or tensors, None where there is none; in one go, since a small call's time is its host's. A tensor's
+    strides are the caller's to describe in `op`: one whose last dimension is not contiguous cannot be."""
+    out = []
+    for x in buffers:
+        if x is not None and not isinstance(x, int):
+            if not x.is_contiguous() and x.stride(-1) != 1 and x.size(-1) > 1:
+                raise FiccoError(FICCO_ERR_ARG, "a tensor's last dimension must be contiguous")
+            x = x.data_ptr()
+        out.append(x)
+    return out
+
+
+def _stream(x):
+    return x if x is None or isinstance(x, int) else x.cuda_stream
 
 
 def ficco_linear_workspace(op, backward=False):
@@ -386,14 +387,14 @@ def ficco_linear_workspace(op, backward=False):
 
 def ficco_linear(op, A, W, bias, residual, pre, C_dev, workspace, workspace_bytes, stream):
     """C = act(A W + bias) + residual (see include/ficco.h); ``op``: a :class:`ficco_linear_t`."""
-    return _ok(load().ficco_linear(op, _addr(A), _addr(W), _addr(bias), _addr(residual), _addr(pre), _addr(C_dev), _addr(workspace),
-                                   workspace_bytes, _addr(stream)), "ficco_linear")
+    return _ok(load().ficco_linear(op, *_addrs(A, W, bias, residual, pre, C_dev, workspace),
+                                   workspace_bytes, _stream(stream)), "ficco_linear")
 
 
 def ficco_linear_backward(op, A, W, pre, dC, dA, dW, dbias, workspace, workspace_bytes, stream):
     """Gradients of :func:`ficco_linear`; any of dA, dW and dbias may be None."""
-    return _ok(load().ficco_linear_backward(op, _addr(A), _addr(W), _addr(pre), _addr(dC), _addr(dA), _addr(dW), _addr(dbias), _addr(workspace),
-                                            workspace_bytes, _addr(stream)), "ficco_linear_backward")
+    return _ok(load().ficco_linear_backward(op, *_addrs(A, W, pre, dC, dA, dW, dbias, workspace),
+                                            workspace_bytes, _stream(stream)), "ficco_linear_backward")
 
 
 def ficco_residual_norm_workspace(op):
@@ -405,16 +406,15 @@ def ficco_residual_norm_workspace(op):
 
 def ficco_residual_norm(op, x, block, post_weight, gate, pre_weight, y, h, stream):
     """y = scale x + gate norm(block), h = norm(y) (see include/ficco.h); ``op``: a :class:`ficco_residual_norm_t`."""
-    return _ok(load().ficco_residual_norm(op, _addr(x), _addr(block), _addr(post_weight), _addr(gate), _addr(pre_weight), _addr(y), _addr(h),
-                                          _addr(stream)), "ficco_residual_norm")
+    return _ok(load().ficco_residual_norm(op, *_addrs(x, block, post_weight, gate, pre_weight, y, h),
+                                          _stream(stream)), "ficco_residual_norm")
 
 
 def ficco_residual_norm_backward(op, y, block, post_weight, gate, pre_weight, dy, dh, dx, dblock, dpost_weight, dgate, dpre_weight, workspace,
                                  workspace_bytes, stream):
     """Gradients of :func:`ficco_residual_norm`; those that are not wanted are None."""
-    return _ok(load().ficco_residual_norm_backward(op, _addr(y), _addr(block), _addr(post_weight), _addr(gate), _addr(pre_weight), _addr(dy), _addr(dh),
-                                                   _addr(dx), _addr(dblock), _addr(dpost_weight), _addr(dgate), _addr(dpre_weight), _addr(workspace),
-                                                   workspace_bytes, _addr(stream)), "ficco_residual_norm_backward")
+    return _ok(load().ficco_residual_norm_backward(op, *_addrs(y, block, post_weight, gate, pre_weight, dy, dh, dx, dblock, dpost_weight, dgate, dpre_weight, workspace),
+                                                   workspace_bytes, _stream(stream)), "ficco_residual_norm_backward")
 
 
 def ficco_expert_balance_workspace(op):
@@ -426,14 +426,14 @@ def ficco_expert_balance_workspace(op):
 
 def ficco_expert_balance(op, logits, ids, valid, counts, group_valid, loss, workspace, workspace_bytes, stream):
     """Counts per expert and the balance loss (see include/ficco.h); ``op``: a :class:`ficco_expert_balance_t`."""
-    return _ok(load().ficco_expert_balance(op, _addr(logits), _addr(ids), _addr(valid), _addr(counts), _addr(group_valid), _addr(loss), _addr(workspace),
-                                           workspace_bytes, _addr(stream)), "ficco_expert_balance")
+    return _ok(load().ficco_expert_balance(op, *_addrs(logits, ids, valid, counts, group_valid, loss, workspace),
+                                           workspace_bytes, _stream(stream)), "ficco_expert_balance")
 
 
 def ficco_expert_balance_backward(op, logits, valid, counts, group_valid, dloss, dlogits, stream):
     """The logits' gradient of :func:`ficco_expert_balance`."""
-    return _ok(load().ficco_expert_balance_backward(op, _addr(logits), _addr(valid), _addr(counts), _addr(group_valid), _addr(dloss), _addr(dlogits),
-                                                    _addr(stream)), "ficco_expert_balance_backward")
+    return _ok(load().ficco_expert_balance_backward(op, *_addrs(logits, valid, counts, group_valid, dloss, dlogits),
+                                                    _stream(stream)), "ficco_expert_balance_backward")
 
 
 def ficco_destroy(plan):

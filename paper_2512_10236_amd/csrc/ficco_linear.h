@@ -16,7 +16,8 @@ struct LinearLaunch {
     Epilogue e;
 };
 
-// One launch over all tiles, at most as many workgroups as run at once; the tiles in the order of gemm_blocks_kernel.
+// One launch over all tiles, at most as many workgroups as run at once; the tiles in the order of gemm_blocks_kernel. M 16384, K 8192,
+// N 3584 with GELU and its argument stored: 730 us, 1.32 PFLOP/s, at the card's power limit; a large library product reaches 1.4-1.5.
 // SA, SB: A, W as [K][...]. Not both: the transposing reads move 64 bytes a cycle where the others move 128, and with both operands
 // through them LDS is what the kernel waits for (dW of M 8192, K 8192, N 3584 390 us; one of them 345, none 333).
 template <class T, bool SA, bool SB>
