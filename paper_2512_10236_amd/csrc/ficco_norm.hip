@@ -192,15 +192,16 @@ static __device__ __forceinline__ Vec8 widen_raw(const u32x4_t (&r)[F32 ? 2 : 1]
 // and writes them once: sums over rows in a fixed order, without atomics. A row needs two sums over its columns in turn, the
 // second of what the first gives, so the next row is loaded before the first: its way from memory is then behind both. What a
 // thread past the row's end loads is the row's first vector, and nothing comes of it. 16384 rows of 4096 in bf16, all gradients:
-// 173 us with the sums, 4.7 TB/s; rows of more than 8192 values reach 3.
+// 173 us with the sums, 4.7 TB/s.
 template <int TPR, int V, bool F32>
 __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), (V == 1 ? 4 : 2)) void residual_norm_backward_kernel(NormLaunch a)
 {
     typedef RowCfg<TPR, V> R;
     constexpr int ROWS = R::ROWS;
-    // One vector a thread: the parameters stay in 128 registers, and the next row is loaded early. Two: neither has room, and of
-    // the three partial sums two lie in LDS ([2][V][2][TPR] four floats each; with all three in registers 16384 values a row
-    // spilled and reached 2.0 TB/s).
+    // One vector a thread: the parameters stay in 128 registers, and the next row is loaded early. Four, of longer rows: neither has
+    // room in 256, and of the three partial sums two lie in LDS ([2][V][2][TPR] four floats each). 512 threads with four rather than
+    // 1024 with two: what a thread has beside its values is there once for four, and nothing spills (3000 rows of 16384 in bf16
+    // 162 us, 3.6 TB/s, against 179; one row 11 against 13).
     constexpr bool KEEP = V == 1;
     extern __shared__ f32x4_t s_acc[];
     __shared__ float s_a[2][3 * 16], s_b[2][16];      // in turns, so that a row's places are not those a slower wavefront still reads
@@ -256,11 +257,22 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), (V == 1 ? 4 : 2)) void r
     }
     auto param = [&](const Vec8 &kept, const void *from, int64_t at) __attribute__((always_inline)) {
         if constexpr (KEEP) return kept;
-        else return from ? param8(from, a.param_f32, at) : Vec8{};
+        else {
+            asm volatile("" : "+v"(at));   // not moved out of the loop over the rows
+            return from ? param8(from, a.param_f32, at) : Vec8{};
+        }
     };
     // without KEEP: one vector's values at a time
     auto apart = [&]() __attribute__((always_inline)) {
         if constexpr (!KEEP) __builtin_amdgcn_sched_barrier(0);
+    };
+    // ... and its values as they came, to be widened anew: else the compiler keeps them widened from one use to the next
+    auto as_they_came = [&](RawRow<F32> &raw) __attribute__((always_inline)) {
+        if constexpr (!KEEP) {
+#pragma unroll
+            for (int k = 0; k < (F32 ? 2 : 1); ++k) asm volatile("" : "+v"(raw.y[k]), "+v"(raw.dy[k]));
+            asm volatile("" : "+v"(raw.b), "+v"(raw.dh));
+        }
     };
     auto load = [&](RawRow<F32> &raw, int64_t row, int v) __attribute__((always_inline)) {
         const int64_t at = row * a.width + col[v];
@@ -303,6 +315,7 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), (V == 1 ? 4 : 2)) void r
             }
 #pragma unroll
             for (int k = 0; k < 3; ++k) s[k] += there[v] != 0.f ? t[k] : 0.f;
+            as_they_came(now[v]);
             apart();
         }
         if (KEEP && row + 1 < end) load(next, row + 1, 0);
@@ -353,6 +366,7 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), (V == 1 ? 4 : 2)) void r
                 s4[0] += in ? sum : 0.f;
                 add(kept_post, 0, v, t);
             }
+            as_they_came(now[v]);
             apart();
         }
         if (post) thread_sums<TPR, 1>(s4, s_b[parity]);
@@ -517,7 +531,7 @@ int launch_backward(const NormLaunch &a, bool f32, hipStream_t s)
     case 512: return launch_backward_t<512, 1>(a, f32, s);
     case 768: return launch_backward_t<768, 1>(a, f32, s);
     }
-    return a.width <= 8192 ? launch_backward_t<1024, 1>(a, f32, s) : launch_backward_t<1024, 2>(a, f32, s);
+    return a.width <= 8192 ? launch_backward_t<1024, 1>(a, f32, s) : launch_backward_t<512, 4>(a, f32, s);
 }
 
 int forward(const ficco_residual_norm_t *op, const void *x, const void *block, const void *post, const void *gate, const void *pre, void *y, void *h,
