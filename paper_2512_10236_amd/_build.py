@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libficco.so")
 SOURCES = ["ficco_gemm.hip", "ficco_reduce.hip", "ficco_plan.hip", "ficco_engines.hip", "ficco_api.hip", "ficco_static.hip", "ficco_direct.hip",
            "ficco_linear.hip", "ficco_linear_strided.hip", "ficco_norm.hip", "ficco_balance.hip"]
-HEADERS = ["ficco_internal.h", "ficco_gate.h", "ficco_mfma.h", "ficco_tile.h", "ficco_plan.h", "ficco_epilogue.h", "ficco_operators.h", "ficco_linear.h", "ficco_lanes.h",
+HEADERS = ["ficco_internal.h", "ficco_gate.h", "ficco_mfma.h", "ficco_tile.h", "ficco_plan.h", "ficco_epilogue.h", "ficco_operators.h", "ficco_linear.h", "ficco_lanes.h", "ficco_token_run.h",
            os.path.join("..", "..", "include", "ficco.h")]
 
 # packed fp32 instructions are switched off for all device code (some of their forms have given wrong results on this hardware)

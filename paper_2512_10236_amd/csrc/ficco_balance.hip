@@ -8,6 +8,7 @@
 #include "ficco_operators.h"
 #include "ficco_epilogue.h"
 #include "ficco_lanes.h"
+#include "ficco_token_run.h"
 
 namespace ficco {
 namespace {
@@ -27,7 +28,7 @@ struct BalanceLaunch {
     int32_t n_terms;
     int64_t ld;
     int32_t tokens, group_tokens, groups, experts, top_k;
-    int32_t per_group, chunk_tokens;       // chunk c: the (c % per_group)-th run of chunk_tokens tokens of group c / per_group
+    int32_t per_group, chunk_tokens;       // see token_run
     float coefficient;
 };
 
@@ -89,13 +90,9 @@ static __device__ __forceinline__ float group_scale(const BalanceLaunch &a, int 
     return n > 0 ? a.coefficient * (float)a.experts / ((float)a.groups * (float)a.top_k * (float)n * (float)n) : 0.f;
 }
 
-static __device__ __forceinline__ void chunk_range(const BalanceLaunch &a, int chunk, int &group, int &begin, int &end)
+static __device__ __forceinline__ TokenRun chunk_run(const BalanceLaunch &a, int chunk)
 {
-    group = chunk / a.per_group;
-    const int64_t b = (int64_t)group * a.group_tokens + (int64_t)(chunk % a.per_group) * a.chunk_tokens;
-    const int64_t e = min(min(b + a.chunk_tokens, (int64_t)(group + 1) * a.group_tokens), (int64_t)a.tokens);
-    begin = (int)min(b, (int64_t)a.tokens);
-    end = (int)max(e, (int64_t)begin);
+    return token_run(chunk, a.per_group, a.chunk_tokens, a.group_tokens, a.tokens);
 }
 
 // The probabilities of a token, in place of its logits. A token whose logits are all -inf has none.
@@ -119,16 +116,17 @@ static __device__ __forceinline__ void softmax(float (&x)[V])
     for (int v = 0; v < V; ++v) x[v] *= r;
 }
 
-// Calls f(token, probabilities) for the tokens [begin, end) of a workgroup's share, LANES lanes a token and TOKENS of them at a time, so that their
+// Calls f(token, probabilities) for the tokens of a workgroup's run, LANES lanes a token and TOKENS of them at a time, so that their
 // loads are in flight together. Padding, and what is behind the end, has no probabilities; its logits are not read.
 template <class L, int LANES, int V, bool FOURS, class Fn>
-static __device__ __forceinline__ void for_tokens(const BalanceLaunch &a, int begin, int end, Fn &&f)
+static __device__ __forceinline__ void for_tokens(const BalanceLaunch &a, const TokenRun &run, Fn &&f)
 {
     typedef Spread<LANES, V, FOURS> S;
     constexpr int SUBS = 256 / LANES, T = S::TOKENS;
     const int lane = threadIdx.x % LANES, sub = LANES == 64 ? scalar(threadIdx.x / 64) : threadIdx.x / LANES;
     const L *logits = static_cast<const L *>(a.logits);
-    int64_t first = begin + sub;
+    const int64_t end = run.end;
+    int64_t first = run.begin + sub;
     int use[T];
     auto look = [&](int64_t t0) __attribute__((always_inline)) {
 #pragma unroll
@@ -181,18 +179,18 @@ __global__ __launch_bounds__(256) void balance_kernel(BalanceLaunch a)
     __shared__ int s_n;
     int *const s_c = reinterpret_cast<int *>(s_p + SUBS * LANES * V);
     const int E = a.experts;
-    int group, begin, end;
-    chunk_range(a, blockIdx.x, group, begin, end);
+    const TokenRun run = chunk_run(a, blockIdx.x);
+    const int group = run.group;
     for (int e = threadIdx.x; e < E; e += 256) s_c[e] = 0;
     if (threadIdx.x == 0) s_n = 0;
     __syncthreads();
-    for (int64_t i = (int64_t)begin * a.top_k + threadIdx.x; i < (int64_t)end * a.top_k; i += 256) {
+    for (int64_t i = run.begin * a.top_k + threadIdx.x; i < run.end * a.top_k; i += 256) {
         const int id = a.ids[i];
         if ((unsigned)id < (unsigned)E && (!a.valid || a.valid[i / a.top_k])) atomicAdd(s_c + id, 1);
     }
     if (a.valid) {
         int n = 0;
-        for (int t = begin + (int)threadIdx.x; t < end; t += 256) n += a.valid[t] != 0;
+        for (int64_t t = run.begin + threadIdx.x; t < run.end; t += 256) n += a.valid[t] != 0;
         if (n) atomicAdd(&s_n, n);
     }
     if (a.loss) {
@@ -200,7 +198,7 @@ __global__ __launch_bounds__(256) void balance_kernel(BalanceLaunch a)
         float p[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) p[v] = 0.f;
-        for_tokens<L, LANES, V, FOURS>(a, begin, end, [&](int64_t, const float (&x)[V]) __attribute__((always_inline)) {
+        for_tokens<L, LANES, V, FOURS>(a, run, [&](int64_t, const float (&x)[V]) __attribute__((always_inline)) {
 #pragma unroll
             for (int v = 0; v < V; ++v) p[v] += x[v];
         });
@@ -208,7 +206,7 @@ __global__ __launch_bounds__(256) void balance_kernel(BalanceLaunch a)
         for (int v = 0; v < V; ++v) s_p[sub * LANES * V + S::expert(lane, v)] = p[v];
     }
     __syncthreads();
-    const int n = a.valid ? s_n : end - begin;
+    const int n = a.valid ? s_n : (int)(run.end - run.begin);
     float term = 0.f;
     for (int e = threadIdx.x; e < E; e += 256) {
         float t = 0.f;
@@ -302,8 +300,8 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(BalanceLaunch a)
 {
     typedef Spread<LANES, V, FOURS> S;
     const int E = a.experts, lane = threadIdx.x % LANES;
-    int group, begin, end;
-    chunk_range(a, blockIdx.x, group, begin, end);
+    const TokenRun run = chunk_run(a, blockIdx.x);
+    const int group = run.group;
     int c[V], total = 0;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -318,14 +316,14 @@ __global__ __launch_bounds__(256) void balance_backward_kernel(BalanceLaunch a)
     for (int v = 0; v < V; ++v) dist[v] = (float)((int64_t)c[v] * E - total);
     const float scale = group_scale(a, a.group_valid[group]) / (float)E * (a.dloss ? a.dloss[0] : 1.0f);
     L *dlogits = static_cast<L *>(a.dlogits);
-    for_tokens<L, LANES, V, FOURS>(a, begin, end, [&](int64_t t, const float (&x)[V]) __attribute__((always_inline)) {
+    for_tokens<L, LANES, V, FOURS>(a, run, [&](int64_t t, const float (&x)[V]) __attribute__((always_inline)) {
         float mean = 0.f, d[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) mean = fmaf(x[v], dist[v], mean);
         mean = lane_sum<LANES>(mean);
 #pragma unroll
         for (int v = 0; v < V; ++v) d[v] = scale * x[v] * (dist[v] - mean);
-        if (t < end) S::store(d, dlogits + t * a.ld, lane, E);
+        if (t < run.end) S::store(d, dlogits + t * a.ld, lane, E);
     });
 }
 
