@@ -360,18 +360,77 @@ def ficco_ideal_overlap_us(t_comm_us, t_gemm_us, n):
     return float(load().ficco_ideal_overlap_us(t_comm_us, t_gemm_us, n))
 
 
-# ---- operators around the pair: `op` is the struct of the C interface, tensors have to be laid out as it says
-def _addrs(*buffers):
-    """Addresses of buffers or tensors, None where there is none; in one go, since a small call's time is its host's. A tensor's
-    strides are the caller's to describe in `op`: one whose last dimension is not contiguous cannot be."""
-    out = []
-    for x in buffers:
-        if x is not None and not isinstance(x, int):
-            if not x.is_contiguous() and x.stride(-1) != 1 and x.size(-1) > 1:
-                raise FiccoError(FICCO_ERR_ARG, "a tensor's last dimension must be contiguous")
-            x = x.data_ptr()
-        out.append(x)
-    return out
+# ---- operators around the pair: `op` is the struct of the C interface, and a tensor has to be what it says: of that type, in one piece or, where
+# it has a row stride, with rows that far apart. An address (int) is taken as it is, a contiguous tensor of torch.uint8 as memory.
+_BF16, _F32, _INT32, _BYTE = 1, 2, 4, 8
+_TAKEN_AS = {"bfloat16": _BF16, "int16": _BF16, "uint16": _BF16, "float32": _F32, "int32": _F32 | _INT32, "uint32": _F32 | _INT32, "int8": _BYTE, "bool": _BYTE,
+             "uint8": _BF16 | _F32 | _INT32 | _BYTE}
+_taken_as = {}                                           # the same by the types themselves, as they come
+
+
+def _type(x):
+    t = _taken_as.get(x.dtype)
+    if t is None:
+        t = _taken_as[x.dtype] = _TAKEN_AS.get(str(x.dtype).rpartition(".")[2], 0)
+    return t
+
+
+def _refuse(name, why):
+    raise FiccoError(FICCO_ERR_ARG, f"{name} {why}")
+
+
+def _dense(x, kind, name):
+    """Address of an operand that lies in one piece."""
+    if x is None or isinstance(x, int):
+        return x
+    if not _type(x) & kind:
+        _refuse(name, f"is {x.dtype}")
+    if not x.is_contiguous():
+        _refuse(name, "is not contiguous")
+    return x.data_ptr()
+
+
+def _rows(x, kind, rows, width, ld, name):
+    """Address of an operand of rows of `width` elements, `ld` apart (0: dense)."""
+    if x is None or isinstance(x, int):
+        return x
+    if not _type(x) & kind:
+        _refuse(name, f"is {x.dtype}")
+    ld = ld or width
+    if x.is_contiguous():
+        # memory, in whatever shape, but for rows that are not the struct's: a buffer whose stride was left out
+        if rows > 1 and x.dim() > 1 and ld % max(x.size(-1), 1) and x.numel() != rows * ld and not _type(x) & _BYTE:
+            _refuse(name, f"has rows of {x.size(-1)} elements, not {ld}")
+        return x.data_ptr()
+    piece, apart = 1, False                              # elements in one piece, and with `apart` in rows that are as far apart
+    for size, stride in zip(reversed(x.shape), reversed(x.stride())):
+        if size == 1:
+            continue
+        if stride != piece:
+            if piece >= (rows - 1) * ld + width:         # the others are not looked at
+                break
+            if apart or stride != ld or not width <= piece <= ld:
+                _refuse(name, f"has no rows of {width} elements {ld} apart")
+            apart, piece = True, ld
+        piece *= size
+    return x.data_ptr()
+
+
+def _memory(x):
+    if x is None or isinstance(x, int):
+        return x
+    if not x.is_contiguous():
+        _refuse("workspace", "is not contiguous")
+    return x.data_ptr()
+
+
+def _value(ficco_type):
+    return _F32 if ficco_type == FICCO_F32 else _BF16
+
+
+def _struct(op, kind):
+    """The struct itself, of a pointer to one too; where there is none, one for the C function's refusal."""
+    return op if isinstance(op, kind) else kind() if op is None else op._obj if hasattr(op, "_obj") else op.contents
 
 
 def _stream(x):
@@ -387,14 +446,20 @@ def ficco_linear_workspace(op, backward=False):
 
 def ficco_linear(op, A, W, bias, residual, pre, C_dev, workspace, workspace_bytes, stream):
     """C = act(A W + bias) + residual (see include/ficco.h); ``op``: a :class:`ficco_linear_t`."""
-    return _ok(load().ficco_linear(op, *_addrs(A, W, bias, residual, pre, C_dev, workspace),
-                                   workspace_bytes, _stream(stream)), "ficco_linear")
+    o = _struct(op, ficco_linear_t)
+    M, N = o.M, o.N
+    return _ok(load().ficco_linear(op, _rows(A, _BF16, M, o.K, o.lda, "A"), _dense(W, _BF16, "W"), _dense(bias, _value(o.bias_type), "bias"),
+                                   _rows(residual, _BF16, M, N, o.ld_residual, "residual"), _rows(pre, _BF16, M, N, o.ld_pre, "pre"), _rows(C_dev, _BF16, M, N, o.ldc, "C"),
+                                   _memory(workspace), workspace_bytes, _stream(stream)), "ficco_linear")
 
 
 def ficco_linear_backward(op, A, W, pre, dC, dA, dW, dbias, workspace, workspace_bytes, stream):
     """Gradients of :func:`ficco_linear`; any of dA, dW and dbias may be None."""
-    return _ok(load().ficco_linear_backward(op, *_addrs(A, W, pre, dC, dA, dW, dbias, workspace),
-                                            workspace_bytes, _stream(stream)), "ficco_linear_backward")
+    o = _struct(op, ficco_linear_t)
+    M, N = o.M, o.N
+    return _ok(load().ficco_linear_backward(op, _rows(A, _BF16, M, o.K, o.lda, "A"), _dense(W, _BF16, "W"), _rows(pre, _BF16, M, N, o.ld_pre, "pre"), _rows(dC, _BF16, M, N, o.ldc, "dC"),
+                                            _dense(dA, _BF16, "dA"), _dense(dW, _BF16, "dW"), _dense(dbias, _F32, "dbias"), _memory(workspace), workspace_bytes, _stream(stream)),
+               "ficco_linear_backward")
 
 
 def ficco_residual_norm_workspace(op):
@@ -406,15 +471,21 @@ def ficco_residual_norm_workspace(op):
 
 def ficco_residual_norm(op, x, block, post_weight, gate, pre_weight, y, h, stream):
     """y = scale x + gate norm(block), h = norm(y) (see include/ficco.h); ``op``: a :class:`ficco_residual_norm_t`."""
-    return _ok(load().ficco_residual_norm(op, *_addrs(x, block, post_weight, gate, pre_weight, y, h),
-                                          _stream(stream)), "ficco_residual_norm")
+    o = _struct(op, ficco_residual_norm_t)
+    stream_type, param = _value(o.stream_type), _value(o.param_type)
+    return _ok(load().ficco_residual_norm(op, _dense(x, stream_type, "x"), _dense(block, _BF16, "block"), _dense(post_weight, param, "post_weight"), _dense(gate, param, "gate"),
+                                          _dense(pre_weight, param, "pre_weight"), _dense(y, stream_type, "y"), _dense(h, _BF16, "h"), _stream(stream)), "ficco_residual_norm")
 
 
 def ficco_residual_norm_backward(op, y, block, post_weight, gate, pre_weight, dy, dh, dx, dblock, dpost_weight, dgate, dpre_weight, workspace,
                                  workspace_bytes, stream):
     """Gradients of :func:`ficco_residual_norm`; those that are not wanted are None."""
-    return _ok(load().ficco_residual_norm_backward(op, *_addrs(y, block, post_weight, gate, pre_weight, dy, dh, dx, dblock, dpost_weight, dgate, dpre_weight, workspace),
-                                                   workspace_bytes, _stream(stream)), "ficco_residual_norm_backward")
+    o = _struct(op, ficco_residual_norm_t)
+    stream_type, param = _value(o.stream_type), _value(o.param_type)
+    return _ok(load().ficco_residual_norm_backward(op, _dense(y, stream_type, "y"), _dense(block, _BF16, "block"), _dense(post_weight, param, "post_weight"), _dense(gate, param, "gate"),
+                                                   _dense(pre_weight, param, "pre_weight"), _dense(dy, stream_type, "dy"), _dense(dh, _BF16, "dh"), _dense(dx, stream_type, "dx"),
+                                                   _dense(dblock, _BF16, "dblock"), _dense(dpost_weight, _F32, "dpost_weight"), _dense(dgate, _F32, "dgate"),
+                                                   _dense(dpre_weight, _F32, "dpre_weight"), _memory(workspace), workspace_bytes, _stream(stream)), "ficco_residual_norm_backward")
 
 
 def ficco_expert_balance_workspace(op):
@@ -426,13 +497,18 @@ def ficco_expert_balance_workspace(op):
 
 def ficco_expert_balance(op, logits, ids, valid, counts, group_valid, loss, workspace, workspace_bytes, stream):
     """Counts per expert and the balance loss (see include/ficco.h); ``op``: a :class:`ficco_expert_balance_t`."""
-    return _ok(load().ficco_expert_balance(op, *_addrs(logits, ids, valid, counts, group_valid, loss, workspace),
-                                           workspace_bytes, _stream(stream)), "ficco_expert_balance")
+    o = _struct(op, ficco_expert_balance_t)
+    return _ok(load().ficco_expert_balance(op, _rows(logits, _value(o.logits_type), o.tokens, o.experts, o.ld_logits, "logits"), _dense(ids, _INT32, "ids"), _dense(valid, _BYTE, "valid"),
+                                           _dense(counts, _INT32, "counts"), _dense(group_valid, _INT32, "group_valid"), _dense(loss, _F32, "loss"),
+                                           _memory(workspace), workspace_bytes, _stream(stream)), "ficco_expert_balance")
 
 
 def ficco_expert_balance_backward(op, logits, valid, counts, group_valid, dloss, dlogits, stream):
     """The logits' gradient of :func:`ficco_expert_balance`."""
-    return _ok(load().ficco_expert_balance_backward(op, *_addrs(logits, valid, counts, group_valid, dloss, dlogits),
+    o = _struct(op, ficco_expert_balance_t)
+    value = _value(o.logits_type)
+    return _ok(load().ficco_expert_balance_backward(op, _rows(logits, value, o.tokens, o.experts, o.ld_logits, "logits"), _dense(valid, _BYTE, "valid"), _dense(counts, _INT32, "counts"),
+                                                    _dense(group_valid, _INT32, "group_valid"), _dense(dloss, _F32, "dloss"), _rows(dlogits, value, o.tokens, o.experts, o.ld_logits, "dlogits"),
                                                     _stream(stream)), "ficco_expert_balance_backward")
 
 
