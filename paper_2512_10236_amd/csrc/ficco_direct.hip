@@ -221,9 +221,8 @@ typedef DirectCfg<4, 4> D64;
 template <class T, class Extra>
 hipError_t launch_direct_t(const DirectLaunch &a, const Extra &extra, hipStream_t s)
 {
-    static hipError_t once = hipFuncSetAttribute(reinterpret_cast<const void *>(&gemm_direct_kernel<T, Extra>),
-                                                 hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES);
-    if (once != hipSuccess) return once;
+    const hipError_t limit = raise_lds_limit<&gemm_direct_kernel<T, Extra>>(T::LDS_BYTES);
+    if (limit != hipSuccess) return limit;
     DirectLaunch b = a;
     b.tiles_m = (a.M + T::BM - 1) / T::BM;
     b.tiles_n = (a.N + T::BN - 1) / T::BN;

@@ -554,16 +554,10 @@ TileShape tile_shape(int tile)
 }
 
 template <class T>
-static hipError_t set_lds_limit(const void *fn)
-{
-    return hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES);
-}
-
-template <class T>
 static hipError_t launch_gemm_t(const GemmLaunch &a, hipStream_t s)
 {
-    static hipError_t once = set_lds_limit<T>(reinterpret_cast<const void *>(&gemm_blocks_kernel<T>));
-    if (once != hipSuccess) return once;
+    const hipError_t limit = raise_lds_limit<&gemm_blocks_kernel<T>>(T::LDS_BYTES);
+    if (limit != hipSuccess) return limit;
     const int tiles_n = (a.N + T::BN - 1) / T::BN;
     const int rt = (a.rows_per_block + T::BM - 1) / T::BM;
     const int64_t total = (int64_t)a.n_blocks * rt * tiles_n;
@@ -606,10 +600,8 @@ static hipError_t launch_gemm_t(const GemmLaunch &a, hipStream_t s)
 template <class T>
 static hipError_t launch_resident_t(const ResidentLaunch &r, hipStream_t s)
 {
-    static hipError_t once = set_lds_limit<T>(reinterpret_cast<const void *>(&gemm_resident_kernel<T, false>));
-    static hipError_t once_out = set_lds_limit<T>(reinterpret_cast<const void *>(&gemm_resident_kernel<T, true>));
-    if (once != hipSuccess) return once;
-    if (once_out != hipSuccess) return once_out;
+    const hipError_t limit = r.done_count ? raise_lds_limit<&gemm_resident_kernel<T, true>>(T::LDS_BYTES) : raise_lds_limit<&gemm_resident_kernel<T, false>>(T::LDS_BYTES);
+    if (limit != hipSuccess) return limit;
     if (r.grid <= 0 || r.g.lda > kMaxK || r.g.K > kMaxK) return hipErrorInvalidValue;
     if (r.done_count)
         hipLaunchKernelGGL((gemm_resident_kernel<T, true>), dim3((unsigned)r.grid), dim3(T::THREADS), T::LDS_BYTES, s, r);
@@ -621,8 +613,8 @@ static hipError_t launch_resident_t(const ResidentLaunch &r, hipStream_t s)
 template <class T>
 static hipError_t launch_resident2d_t(const Resident2DLaunch &r, hipStream_t s)
 {
-    static hipError_t once = set_lds_limit<T>(reinterpret_cast<const void *>(&gemm_resident2d_kernel<T>));
-    if (once != hipSuccess) return once;
+    const hipError_t limit = raise_lds_limit<&gemm_resident2d_kernel<T>>(T::LDS_BYTES);
+    if (limit != hipSuccess) return limit;
     if (r.grid <= 0 || !r.k0 || r.g.K > kMaxK) return hipErrorInvalidValue;
     hipLaunchKernelGGL(gemm_resident2d_kernel<T>, dim3((unsigned)r.grid), dim3(T::THREADS), T::LDS_BYTES, s, r);
     return hipGetLastError();
@@ -631,8 +623,7 @@ static hipError_t launch_resident2d_t(const Resident2DLaunch &r, hipStream_t s)
 template <class T>
 static int resident2d_grid_t(int device)
 {
-    static hipError_t once = set_lds_limit<T>(reinterpret_cast<const void *>(&gemm_resident2d_kernel<T>));
-    (void)once;
+    (void)raise_lds_limit<&gemm_resident2d_kernel<T>>(T::LDS_BYTES);
     int per_cu = 0, cus = 0;
     if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, gemm_resident2d_kernel<T>, T::THREADS, T::LDS_BYTES) != hipSuccess) return 0;
     if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess) return 0;
@@ -642,8 +633,8 @@ static int resident2d_grid_t(int device)
 template <class T>
 static hipError_t launch_grouped_t(const GroupedLaunch &r, hipStream_t s)
 {
-    static hipError_t once = set_lds_limit<T>(reinterpret_cast<const void *>(&gemm_grouped_kernel<T>));
-    if (once != hipSuccess) return once;
+    const hipError_t limit = raise_lds_limit<&gemm_grouped_kernel<T>>(T::LDS_BYTES);
+    if (limit != hipSuccess) return limit;
     if (r.grid <= 0 || r.n_row_tiles <= 0 || r.g.lda > kMaxK || r.g.K > kMaxK) return hipErrorInvalidValue;
     hipLaunchKernelGGL(gemm_grouped_kernel<T>, dim3((unsigned)r.grid), dim3(T::THREADS), T::LDS_BYTES, s, r);
     return hipGetLastError();
@@ -652,8 +643,7 @@ static hipError_t launch_grouped_t(const GroupedLaunch &r, hipStream_t s)
 template <class T>
 static int grouped_grid_t(int device)
 {
-    static hipError_t once = set_lds_limit<T>(reinterpret_cast<const void *>(&gemm_grouped_kernel<T>));
-    (void)once;
+    (void)raise_lds_limit<&gemm_grouped_kernel<T>>(T::LDS_BYTES);
     int per_cu = 0, cus = 0;
     if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, gemm_grouped_kernel<T>, T::THREADS, T::LDS_BYTES) != hipSuccess) return 0;
     if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess) return 0;
@@ -663,8 +653,7 @@ static int grouped_grid_t(int device)
 template <class T>
 static int resident_grid_t(int device)
 {
-    static hipError_t once = set_lds_limit<T>(reinterpret_cast<const void *>(&gemm_resident_kernel<T, false>));
-    (void)once;
+    (void)raise_lds_limit<&gemm_resident_kernel<T, false>>(T::LDS_BYTES);
     int per_cu = 0, cus = 0;
     // (the output-streaming form may need more registers, but every tile shape is limited by LDS first)
     if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, gemm_resident_kernel<T, false>, T::THREADS, T::LDS_BYTES) != hipSuccess) return 0;

@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
+
 namespace ficco {
 
 // Workgroup tile shapes. The k order (ascending, 32 at a time inside one 16x16x32 MFMA) is the
@@ -363,6 +365,18 @@ hipError_t launch_direct(int row_blocks, const DirectLaunch &a, hipStream_t s);
 // The same with the linear operator's epilogue (ficco_epilogue.h) and with rows of A and C at strides of their own.
 struct Epilogue;
 hipError_t launch_direct_epilogue(int row_blocks, const DirectLaunch &a, const Epilogue &e, int64_t lda, int64_t ldc, hipStream_t s);
+// Raises a kernel's limit of dynamic LDS, which is the device's: once on every device that the kernel is launched on.
+template <auto *KERNEL>
+hipError_t raise_lds_limit(int bytes)
+{
+    static std::atomic<bool> raised[64];
+    int dev = 0;
+    hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess || (dev < 64 && raised[dev].load(std::memory_order_relaxed))) return e;
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess && dev < 64) raised[dev].store(true, std::memory_order_relaxed);
+    return e;
+}
 // W[K,N] -> Wt[N,K]; also clears up to 256 words at `clear`
 hipError_t launch_pack_weight(const uint16_t *W, uint16_t *Wt, int64_t K, int64_t N, hipStream_t s, uint32_t *clear = nullptr, int clear_words = 0);
 int resident_grid_size(int tile, int device);

@@ -73,7 +73,7 @@ int launch_tiles_t(const LinearLaunch &a, hipStream_t s)
     if (fit == 0) {
         const auto fn = &linear_tiles_kernel<T, SA, SB>;
         int per_cu = 0;
-        HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES));
+        HIP_TRY((raise_lds_limit<&linear_tiles_kernel<T, SA, SB>>(T::LDS_BYTES)));
         HIP_TRY(hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, fn, T::THREADS, T::LDS_BYTES));
         fit = std::max(8, per_cu * compute_units() / 8 * 8);
         if (dev < 64) fit_of[dev] = fit;

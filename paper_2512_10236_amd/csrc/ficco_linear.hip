@@ -218,13 +218,7 @@ int launch_rows_t(const LinearLaunch &a, int splits, float *part, hipStream_t s)
 {
     const int64_t tiles = (((int64_t)a.M + T::BM - 1) / T::BM) * (((int64_t)a.N + T::BN - 1) / T::BN) * splits;
     if (splits < 1 || (splits > 1 && !part) || tiles > 0x7FFFFFFF / kRowsThreads) return FICCO_ERR_SHAPE;
-    static bool set[64];                   // per device
-    int dev = 0;
-    HIP_TRY(hipGetDevice(&dev));
-    if (dev >= 64 || !set[dev]) {
-        HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(&linear_rows_kernel<T>), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS_BYTES));
-        if (dev < 64) set[dev] = true;
-    }
+    HIP_TRY(raise_lds_limit<&linear_rows_kernel<T>>(T::LDS_BYTES));
     hipLaunchKernelGGL(linear_rows_kernel<T>, dim3((unsigned)tiles), dim3(kRowsThreads), T::LDS_BYTES, s, a, splits, part);
     HIP_TRY(hipGetLastError());
     if (splits > 1) {

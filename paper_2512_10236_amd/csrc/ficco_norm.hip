@@ -514,7 +514,7 @@ int launch_backward_t(const NormLaunch &a, bool f32, hipStream_t s)
     const dim3 grid((unsigned)((a.chunks + R::ROWS - 1) / R::ROWS)), block(R::THREADS);
     constexpr int LDS = V == 1 ? 0 : 2 * V * 2 * TPR * 16;
     const auto fn = f32 ? &residual_norm_backward_kernel<TPR, V, true> : &residual_norm_backward_kernel<TPR, V, false>;
-    if (LDS) HIP_TRY(hipFuncSetAttribute(reinterpret_cast<const void *>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, LDS));
+    if (LDS) HIP_TRY((f32 ? raise_lds_limit<&residual_norm_backward_kernel<TPR, V, true>>(LDS) : raise_lds_limit<&residual_norm_backward_kernel<TPR, V, false>>(LDS)));
     hipLaunchKernelGGL(fn, grid, block, LDS, s, a);
     HIP_TRY(hipGetLastError());
     return FICCO_OK;
