@@ -1,6 +1,9 @@
 """How the operators launch their kernels, seen on the host (tests/standin.py)."""
+import re
+
 import pytest
 
+import linear_pool
 import standin
 
 DEFAULT_LDS = 64 * 1024          # what a launch may ask for without raising the kernel's limit
@@ -32,3 +35,14 @@ def test_lds_limits_are_raised_on_every_device(lib):
     for what in ("gemm_direct_kernel", "linear_rows_kernel", "linear_tiles_kernel", "gemm_blocks_kernel", "residual_norm_backward_kernel"):
         assert {l.device for l in large if l.kernel.startswith(what)} == {0, 1, 3}, what
     assert not sorted({(l.kernel, l.device) for l in large if l.limit < l.lds})
+
+
+def test_every_kernel_of_the_linear_operator_is_reached(lib):
+    """... by a call of the pool that tests/test_gpu_linear_kernels.py draws its calls from; a kernel that no size takes has no place in the library."""
+    by = linear_pool.reached(lib)
+    assert len(by) > 40
+    assert not [k for k, calls in by.items() if not calls and linear_pool.of_the_operator(k)]
+    for kernel, calls in by.items():
+        if kernel.startswith("linear_tiles_kernel"):
+            columns = int(re.search(r"TileCfg<\d+, (\d+)", kernel).group(1))
+            assert any(c["fields"]["N"] % columns for c in calls), kernel
