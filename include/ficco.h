@@ -542,7 +542,7 @@ int ficco_gemm_static(int64_t M, int64_t K, int64_t N, const void *A_dev, const 
  * the caller may capture it into a graph. A workspace is device memory of the caller's, of at least the bytes that the
  * operator's _workspace function gives for the same struct (NULL where that is 0); it holds nothing between calls, and
  * calls that may run at the same time need one each. All matrices are row-major. Every pointer must be device memory of
- * the current device (FICCO_ERR_ARG), and those of bf16 matrices and of workspaces 16-byte aligned, other 32-bit values 4-byte (FICCO_ERR_ARG).
+ * the current device and aligned as its operator says, a workspace to 16 bytes (FICCO_ERR_ARG).
  * Inputs and outputs must not overlap except where it is said. Each result is rounded once, from fp32 to its type, to
  * nearest even; sums are in fp32 and in an order that depends on the sizes only, so that equal calls give equal bits.
  */
@@ -573,6 +573,7 @@ typedef enum ficco_weight_layout {
  * Row strides in elements, 0 = dense: lda of A, ldc of C and of dC, ld_residual, ld_pre; multiples of 8, at least the row's
  * length and at most 2^22. Shape rules (FICCO_ERR_SHAPE): 0 <= M < 2^31, K % 64 == 0, N % 8 == 0, K and N
  * positive and at most 2^22; the backward pass needs M <= 2^22. With M == 0 nothing is read; dW and dbias are zero.
+ * Alignment: matrices 16 bytes, bias that of its type, dbias 4 bytes.
  * Workspace: the forward of a [K,N] weight keeps there the partial sums of a long k over few rows, or, where neither such a product nor
  * one over whole tiles is the fastest, a re-laid out copy of the weight; the backward keeps dZ and the operands that its
  * products need with another order of their values.
@@ -606,7 +607,8 @@ int ficco_linear_backward(const ficco_linear_t *op, const void *A, const void *W
  *   dblock bf16, and fp32 sums over the rows: dpost_weight [width], dgate of the gate's shape, dpre_weight [width]
  * each given or NULL; those of NULL parameters must be NULL. dpost_weight, dgate and, with post_weight, dblock need block (FICCO_ERR_ARG).
  * Shape rules (FICCO_ERR_SHAPE): 0 <= rows < 2^31, width % 8 == 0, 8 <= width <= 16384, gate_rows >= 0. With no rows
- * nothing is read, and the sums are zero. eps >= 0 and finite (FICCO_ERR_ARG).
+ * nothing is read, and the sums are zero. eps >= 0, eps and residual_scale finite (FICCO_ERR_ARG). Alignment: 16 bytes, all operands
+ * of either type.
  */
 typedef struct ficco_residual_norm_t {
     int64_t rows, width, gate_rows;
@@ -638,7 +640,8 @@ int ficco_residual_norm_backward(const ficco_residual_norm_t *op, const void *y,
  * The gradient: dlogits of logits' type and stride = dloss[0] (fp32, NULL: 1) times d loss / d logits, through the
  * probabilities (counts are constants); 0 for padding. It takes counts and group_valid as the forward wrote them. dlogits may be logits itself.
  * Shape rules (FICCO_ERR_SHAPE): 0 <= tokens < 2^31, 1 <= experts <= 1024, 1 <= top_k <= 64, group_tokens >= 0, at most
- * 2^20 groups and 2^31 - 1 slots in each. With no tokens there are no groups: the loss is 0 and nothing else is written.
+ * 2^20 groups and 2^31 - 1 slots in each, ld_logits at most 2^22. With no tokens there are no groups: the loss is 0 and nothing else
+ * is written. coefficient is finite (FICCO_ERR_ARG). Alignment: that of an element, 4 bytes or, of bf16 logits, 2; of valid none.
  */
 typedef struct ficco_expert_balance_t {
     int64_t tokens, group_tokens, ld_logits;

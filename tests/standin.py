@@ -77,32 +77,33 @@ for c in json.load(sys.stdin):
     standin.standin_device(device, cus)
     standin.standin_clear()
     fields, op, given = c["fields"], c["op"], c.get("given", {})
-    at = lambda name: given.get(name, P)
+    each = lambda names: [given.get(name, P) for name in names.split()]
+    ws = lambda n: given.get("workspace", P if n else None)
     try:
         if op == "linear":
             o = F.ficco_linear_t(**fields)
             n = F.ficco_linear_workspace(o)
-            F.ficco_linear(o, P, P, at("bias"), at("residual"), at("pre"), P, P if n else None, n, None)
+            F.ficco_linear(o, *each("A W bias residual pre C"), ws(n), n, None)
         elif op == "linear_backward":
             o = F.ficco_linear_t(**fields)
             n = F.ficco_linear_workspace(o, True)
-            F.ficco_linear_backward(o, P, P, at("pre"), P, at("dA"), at("dW"), at("dbias"), P if n else None, n, None)
+            F.ficco_linear_backward(o, *each("A W pre dC dA dW dbias"), ws(n), n, None)
         elif op == "norm":
             o = F.ficco_residual_norm_t(**fields)
             n = 0
-            F.ficco_residual_norm(o, P, P, at("post"), at("gate"), P, P, P, None)
+            F.ficco_residual_norm(o, *each("x block post gate pre y h"), None)
         elif op == "norm_backward":
             o = F.ficco_residual_norm_t(**fields)
             n = F.ficco_residual_norm_workspace(o)
-            F.ficco_residual_norm_backward(o, P, P, P, P, P, P, P, P, P, P, P, P, P, n, None)
+            F.ficco_residual_norm_backward(o, *each("y block post gate pre dy dh dx dblock dpost dgate dpre"), ws(n), n, None)
         elif op == "balance":
             o = F.ficco_expert_balance_t(**fields)
             n = F.ficco_expert_balance_workspace(o)
-            F.ficco_expert_balance(o, P, P, P, P, P, P, P if n else None, n, None)
+            F.ficco_expert_balance(o, *each("logits ids valid counts group_valid loss"), ws(n), n, None)
         elif op == "balance_backward":
             o = F.ficco_expert_balance_t(**fields)
             n = 0
-            F.ficco_expert_balance_backward(o, P, P, P, P, P, P, None)
+            F.ficco_expert_balance_backward(o, *each("logits valid counts group_valid dloss dlogits"), None)
         status = 0
     except F.FiccoError as e:
         status, n = e.status, -1
