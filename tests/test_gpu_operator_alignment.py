@@ -9,7 +9,7 @@ pytestmark = pytest.mark.gpu
 
 def moved(x, elements):
     """The same values `elements` of theirs behind an aligned address."""
-    out = torch.empty(x.numel() + 16, dtype=x.dtype, device=x.device)[elements:elements + x.numel()].view(x.shape)
+    out = torch.empty(x.numel() + 32, dtype=x.dtype, device=x.device)[elements:elements + x.numel()].view(x.shape)
     return out.copy_(x)
 
 
