@@ -52,15 +52,17 @@ static __device__ __forceinline__ float activate(float z)
     else return z;
 }
 
-// act'(z). Beyond |z| = 32 the smooth ones' slopes are 0 and 1 to the last bit; without the bound z^3 and its exponential would
-// make infinity times zero of large finite values. (NaN passes the comparisons.)
+// act'(z). The smooth ones' slopes are 0 and 1 to the last bit beyond |z| = 32 (GELU, either) or 128 (SiLU, z exp(z) far below zero, which leaves
+// fp32's normal numbers at -91); without the bound z^3 and its exponential, or z itself at infinity, would make infinity times zero of it. (NaN passes
+// the comparisons.)
 template <int ACT>
 static __device__ __forceinline__ float slope(float z)
 {
     if constexpr (ACT == FICCO_ACT_NONE) return 1.0f;
     else if constexpr (ACT == FICCO_ACT_RELU) return z > 0.f ? 1.0f : z != z ? z : 0.f;
     else {
-        z = z > 32.f ? 32.f : z < -32.f ? -32.f : z;
+        constexpr float far = ACT == FICCO_ACT_SILU ? 128.f : 32.f;
+        z = z > far ? far : z < -far ? -far : z;
         if constexpr (ACT == FICCO_ACT_GELU) {
             const float h = normal_tail(z);
             return fmaf(z * 0.39894228f, __builtin_amdgcn_exp2f(z * z * (-0.5f * kLog2E)), z < 0.f ? h : 1.0f - h);
