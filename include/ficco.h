@@ -574,9 +574,9 @@ typedef enum ficco_weight_layout {
  * length and at most 2^22. Shape rules (FICCO_ERR_SHAPE): 0 <= M < 2^31, K % 64 == 0, N % 8 == 0, K and N
  * positive and at most 2^22; the backward pass needs M <= 2^22. With M == 0 nothing is read; dW and dbias are zero.
  * Alignment: matrices 16 bytes, bias that of its type, dbias 4 bytes.
- * Workspace: the forward of a [K,N] weight keeps there the partial sums of a long k over few rows, or, where neither such a product nor
- * one over whole tiles is the fastest, a re-laid out copy of the weight; the backward keeps dZ and the operands that its
- * products need with another order of their values.
+ * Workspace: the forward of a [K,N] weight keeps there the partial sums of a long k over few rows, or, for products whose launch is of parts
+ * of tiles, a re-laid out copy of the weight; the backward keeps dZ and the operands that its products need with another order
+ * of their values.
  */
 typedef struct ficco_linear_t {
     int64_t M, K, N;

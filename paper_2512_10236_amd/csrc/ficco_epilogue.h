@@ -23,8 +23,8 @@ static __device__ __forceinline__ float sigmoid2(float x) { return __builtin_amd
 constexpr float kLog2E = 1.44269504f, kGeluC = 0.7978845608f /* sqrt(2/pi) */, kGeluCube = 0.044715f;
 
 // Phi(-|z|), the normal distribution function's lower tail: erfc(x) exp(x^2), x = |z|/sqrt(2), is smooth in t = 1/(1 + 0.44 x),
-// which maps [0, inf) to (0, 1]; the polynomial is a weighted least-squares fit of its own over x in [0, 10], off by 1.8e-7
-// of the value (the exponent's rounding adds up to 2e-6 at z = -6, where the value is 1e-9).
+// which maps [0, inf) to (0, 1]; the polynomial is a weighted least-squares fit of its own over x in [0, 10], off by 2e-7
+// of the value; in fp32 that is 5e-7 down to z = -1 and, by the exponent's rounding, 2e-6 at -6, where the value is 1e-9, and 3e-6 at -8.
 static __device__ __forceinline__ float normal_tail(float z)
 {
     const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.44f * 0.70710678f, 1.0f));

@@ -276,10 +276,11 @@ RowsTile rows_tile(int64_t M, int64_t K, int64_t N, double us)
 // weight comes from: a CU draws 90-146 KB a us of it from the L2s (40-105 of half lines, the fewer the more CUs do), and from memory 43 (32). A loop over one
 // layer finds a weight of up to 16 MiB in the L2s, a model's layers in turn do not; up to there the rule goes by the geometric mean
 // of both. us, direct / one launch / splits (one layer | layers in turn): M 1, K 4096, N 768 9.0 / 6.5 / 9.0 | 14.5 / 15.8 / 10.3; M 64 of
-// it 9.0 / 7.3 / 9.5 | 15.3 / 14.2 / 11.7; M 3, K 4800, N 560 10.0 / 7.0 / 9.0 | 20.5 / 17.2 / 11.2; beyond 16 MiB M 16, K 8192, N 3584
+// it 9.0 / 9.1 / 9.5 | 15.3 / 14.2 / 11.7; M 3, K 4800, N 560 10.0 / 7.0 / 9.0 | 20.5 / 17.2 / 11.2; beyond 16 MiB M 16, K 8192, N 3584
 // - | 38 / 32 / 20; M 1, K 8192, N 1280 30 / 29 / 13; M 166, K 13184, N 264 50 / - / 19; M 32, K 16384, N 4096 68 / - / 42.
-// Over 110 random products (M to 500, K 1024-16384, N 64-6144) what it takes is 1.4 % slower than the fastest; the direct kernel or a tile
-// throughout 42 %.
+// Over the 110 random products (M to 500, K 1024-16384, N 64-6144) that the rates were fitted to, what it takes is 1.4 % slower than the fastest of
+// these ways; the direct kernel or a tile throughout 42 %. Not in the estimates: that each of the row tiles reads the weight (eight times at M
+// 64, where 8 and 16 rows a tile are estimated alike).
 RowsTile rows_tile_kn(int64_t M, int64_t K, int64_t N, int row_blocks, double us)
 {
     RowsTile best{0, 0, 1};
@@ -499,8 +500,9 @@ int checked(const ficco_linear_t *op, bool backward, ficco_linear_t *out)
     return FICCO_OK;
 }
 
-// How a forward goes: row blocks of the direct kernel, for a small product of a [K,N] weight; or the few-rows kernel's tile, for an
-// [N,K] one; or the tile of the others. These read a [K,N] weight as it is, but parts of tiles need it re-laid out.
+// How a forward goes: row blocks of the direct kernel, for a small product of a [K,N] weight; or the few-rows kernel's tile; or the tile of
+// the others, by the tile rule for operands in place. Whole tiles read a [K,N] weight as it is, but parts of tiles need it re-laid out. That
+// copy is in no estimate (M 198, K 13440, N 2392 83 us a call with it, 53 of an [N,K] weight; M 465, K 14656, N 1112 74, 59).
 struct Forward {
     int row_blocks, tile;
     RowsTile rows;

@@ -201,7 +201,7 @@ __global__ __launch_bounds__((RowCfg<TPR, V>::THREADS), (V == 1 ? 4 : 2)) void r
     // One vector a thread: the parameters stay in 128 registers, and the next row is loaded early. Four, of longer rows: neither has
     // room in 256, and of the three partial sums two lie in LDS ([2][V][2][TPR] four floats each). 512 threads with four rather than
     // 1024 with two: what a thread has beside its values is there once for four, and nothing spills (3000 rows of 16384 in bf16
-    // 162 us, 3.6 TB/s, against 179; one row 11 against 13).
+    // 162 us, 3.7 TB/s, against 179; one row 11 against 13). Narrower rows leave vectors of the four empty: of 12288 137 us, 3.2 TB/s, of 8200 116, 2.5.
     constexpr bool KEEP = V == 1;
     extern __shared__ f32x4_t s_acc[];
     __shared__ float s_a[2][3 * 16], s_b[2][16];      // in turns, so that a row's places are not those a slower wavefront still reads
