@@ -368,23 +368,28 @@ _TAKEN_AS = {"bfloat16": _BF16, "int16": _BF16, "uint16": _BF16, "float32": _F32
 _taken_as = {}                                           # the same by the types themselves, as they come
 
 
-def _type(x):
-    t = _taken_as.get(x.dtype)
-    if t is None:
-        t = _taken_as[x.dtype] = _TAKEN_AS.get(str(x.dtype).rpartition(".")[2], 0)
-    return t
-
-
 def _refuse(name, why):
     raise FiccoError(FICCO_ERR_ARG, f"{name} {why}")
 
 
+def _type(x, kind, name):
+    """What x is taken as, `kind` among it."""
+    t = _taken_as.get(x.dtype)
+    if t is None:
+        t = _taken_as[x.dtype] = _TAKEN_AS.get(str(x.dtype).rpartition(".")[2], 0)
+    if not t & kind:
+        _refuse(name, f"is {x.dtype}")
+    return t
+
+
+# (A small call's time is its host's: the first line of what follows is the usual operand's way.)
 def _dense(x, kind, name):
     """Address of an operand that lies in one piece."""
     if x is None or isinstance(x, int):
         return x
-    if not _type(x) & kind:
-        _refuse(name, f"is {x.dtype}")
+    if _taken_as.get(x.dtype, 0) & kind and x.is_contiguous():
+        return x.data_ptr()
+    _type(x, kind, name)
     if not x.is_contiguous():
         _refuse(name, "is not contiguous")
     return x.data_ptr()
@@ -394,12 +399,14 @@ def _rows(x, kind, rows, width, ld, name):
     """Address of an operand of rows of `width` elements, `ld` apart (0: dense)."""
     if x is None or isinstance(x, int):
         return x
-    if not _type(x) & kind:
-        _refuse(name, f"is {x.dtype}")
     ld = ld or width
-    if x.is_contiguous():
+    whole = x.is_contiguous()
+    if whole and _taken_as.get(x.dtype, 0) & kind and x.numel() == rows * ld:
+        return x.data_ptr()
+    taken = _type(x, kind, name)
+    if whole:
         # memory, in whatever shape, but for rows that are not the struct's: a buffer whose stride was left out
-        if rows > 1 and x.dim() > 1 and ld % max(x.size(-1), 1) and x.numel() != rows * ld and not _type(x) & _BYTE:
+        if rows > 1 and x.dim() > 1 and x.numel() != rows * ld and ld % max(x.size(-1), 1) and not taken & _BYTE:
             _refuse(name, f"has rows of {x.size(-1)} elements, not {ld}")
         return x.data_ptr()
     piece, apart = 1, False                              # elements in one piece, and with `apart` in rows that are as far apart
@@ -446,16 +453,17 @@ def ficco_linear_workspace(op, backward=False):
 
 def ficco_linear(op, A, W, bias, residual, pre, C_dev, workspace, workspace_bytes, stream):
     """C = act(A W + bias) + residual (see include/ficco.h); ``op``: a :class:`ficco_linear_t`."""
-    o = _struct(op, ficco_linear_t)
+    o = op if type(op) is ficco_linear_t else _struct(op, ficco_linear_t)
     M, N = o.M, o.N
     return _ok(load().ficco_linear(op, _rows(A, _BF16, M, o.K, o.lda, "A"), _dense(W, _BF16, "W"), _dense(bias, _value(o.bias_type), "bias"),
-                                   _rows(residual, _BF16, M, N, o.ld_residual, "residual"), _rows(pre, _BF16, M, N, o.ld_pre, "pre"), _rows(C_dev, _BF16, M, N, o.ldc, "C"),
+                                   residual if residual is None else _rows(residual, _BF16, M, N, o.ld_residual, "residual"),
+                                   pre if pre is None else _rows(pre, _BF16, M, N, o.ld_pre, "pre"), _rows(C_dev, _BF16, M, N, o.ldc, "C"),
                                    _memory(workspace), workspace_bytes, _stream(stream)), "ficco_linear")
 
 
 def ficco_linear_backward(op, A, W, pre, dC, dA, dW, dbias, workspace, workspace_bytes, stream):
     """Gradients of :func:`ficco_linear`; any of dA, dW and dbias may be None."""
-    o = _struct(op, ficco_linear_t)
+    o = op if type(op) is ficco_linear_t else _struct(op, ficco_linear_t)
     M, N = o.M, o.N
     return _ok(load().ficco_linear_backward(op, _rows(A, _BF16, M, o.K, o.lda, "A"), _dense(W, _BF16, "W"), _rows(pre, _BF16, M, N, o.ld_pre, "pre"), _rows(dC, _BF16, M, N, o.ldc, "dC"),
                                             _dense(dA, _BF16, "dA"), _dense(dW, _BF16, "dW"), _dense(dbias, _F32, "dbias"), _memory(workspace), workspace_bytes, _stream(stream)),
@@ -471,7 +479,7 @@ def ficco_residual_norm_workspace(op):
 
 def ficco_residual_norm(op, x, block, post_weight, gate, pre_weight, y, h, stream):
     """y = scale x + gate norm(block), h = norm(y) (see include/ficco.h); ``op``: a :class:`ficco_residual_norm_t`."""
-    o = _struct(op, ficco_residual_norm_t)
+    o = op if type(op) is ficco_residual_norm_t else _struct(op, ficco_residual_norm_t)
     stream_type, param = _value(o.stream_type), _value(o.param_type)
     return _ok(load().ficco_residual_norm(op, _dense(x, stream_type, "x"), _dense(block, _BF16, "block"), _dense(post_weight, param, "post_weight"), _dense(gate, param, "gate"),
                                           _dense(pre_weight, param, "pre_weight"), _dense(y, stream_type, "y"), _dense(h, _BF16, "h"), _stream(stream)), "ficco_residual_norm")
@@ -480,7 +488,7 @@ def ficco_residual_norm(op, x, block, post_weight, gate, pre_weight, y, h, strea
 def ficco_residual_norm_backward(op, y, block, post_weight, gate, pre_weight, dy, dh, dx, dblock, dpost_weight, dgate, dpre_weight, workspace,
                                  workspace_bytes, stream):
     """Gradients of :func:`ficco_residual_norm`; those that are not wanted are None."""
-    o = _struct(op, ficco_residual_norm_t)
+    o = op if type(op) is ficco_residual_norm_t else _struct(op, ficco_residual_norm_t)
     stream_type, param = _value(o.stream_type), _value(o.param_type)
     return _ok(load().ficco_residual_norm_backward(op, _dense(y, stream_type, "y"), _dense(block, _BF16, "block"), _dense(post_weight, param, "post_weight"), _dense(gate, param, "gate"),
                                                    _dense(pre_weight, param, "pre_weight"), _dense(dy, stream_type, "dy"), _dense(dh, _BF16, "dh"), _dense(dx, stream_type, "dx"),
@@ -497,7 +505,7 @@ def ficco_expert_balance_workspace(op):
 
 def ficco_expert_balance(op, logits, ids, valid, counts, group_valid, loss, workspace, workspace_bytes, stream):
     """Counts per expert and the balance loss (see include/ficco.h); ``op``: a :class:`ficco_expert_balance_t`."""
-    o = _struct(op, ficco_expert_balance_t)
+    o = op if type(op) is ficco_expert_balance_t else _struct(op, ficco_expert_balance_t)
     return _ok(load().ficco_expert_balance(op, _rows(logits, _value(o.logits_type), o.tokens, o.experts, o.ld_logits, "logits"), _dense(ids, _INT32, "ids"), _dense(valid, _BYTE, "valid"),
                                            _dense(counts, _INT32, "counts"), _dense(group_valid, _INT32, "group_valid"), _dense(loss, _F32, "loss"),
                                            _memory(workspace), workspace_bytes, _stream(stream)), "ficco_expert_balance")
@@ -505,7 +513,7 @@ def ficco_expert_balance(op, logits, ids, valid, counts, group_valid, loss, work
 
 def ficco_expert_balance_backward(op, logits, valid, counts, group_valid, dloss, dlogits, stream):
     """The logits' gradient of :func:`ficco_expert_balance`."""
-    o = _struct(op, ficco_expert_balance_t)
+    o = op if type(op) is ficco_expert_balance_t else _struct(op, ficco_expert_balance_t)
     value = _value(o.logits_type)
     return _ok(load().ficco_expert_balance_backward(op, _rows(logits, value, o.tokens, o.experts, o.ld_logits, "logits"), _dense(valid, _BYTE, "valid"), _dense(counts, _INT32, "counts"),
                                                     _dense(group_valid, _INT32, "group_valid"), _dense(dloss, _F32, "dloss"), _rows(dlogits, value, o.tokens, o.experts, o.ld_logits, "dlogits"),

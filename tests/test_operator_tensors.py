@@ -180,3 +180,11 @@ def test_pointers_to_the_struct(noted):
 def test_no_rows(noted):
     assert call(noted, "linear", F.ficco_linear_t(M=0, K=K, N=N), A=t(0, K), residual=t(0, N), pre=None, C=t(0, N))["pre"] is None
     assert call(noted, "linear", F.ficco_linear_t(M=0, K=K, N=N), A=t(4, 2 * K)[:, :K])
+
+
+def test_a_number(noted):
+    """A tensor without dimensions, as a loss often is."""
+    one = torch.zeros((), dtype=F32)
+    assert call(noted, "balance", loss=one)["loss"] == one.data_ptr()
+    op = F.ficco_expert_balance_t(tokens=1, experts=1, top_k=1, logits_type=F.FICCO_F32)
+    assert call(noted, "balance", op, logits=one)["logits"] == one.data_ptr()
